@@ -352,6 +352,100 @@ int32_t ssm_gather_rows(int32_t batch, int32_t src_rows, int32_t width, const vo
                         const int32_t* d_pos, int32_t n_rows, void* d_dst, void* stream);
 
 /* ------------------------------------------------------------------------ */
+/* 8-bit projections: rows and weights as int8 codes with a scale each.     */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * Codes and scales.  A row y becomes scale = max|y| / 127 (float32) and codes
+ * q = round(y / scale), to nearest even, in [-127, 127], so that q * scale is
+ * within half a step of y.  A row whose largest magnitude is below 2^-100 (a
+ * row of zeros, for one) gets scale 0 and codes 0; a row with an infinity or a
+ * NaN gets scale NaN and codes 0, so that what is computed from it is NaN.
+ * A feed-forward block in 8 bits is
+ *   ssm_norm_i8 -> ssm_gemm_i8 (gate and up weights, one above the other)
+ *   -> ssm_quant_i8 with swiglu -> ssm_gemm_i8 (down) -> ssm_norm_i8 with the
+ * product as the next norm's delta; ssm_quant_i8 also turns weights [out, in]
+ * into codes with a scale for each output channel, once, and attention's
+ * output into the input of its projection.
+ * rows may be 0 (nothing is launched); arrays are contiguous, of any
+ * alignment their type allows.
+ */
+
+/*
+ * RMSNorm with the residual's addition:
+ *   r = d_x + d_delta;  y = r / sqrt(mean(r^2) + eps) * d_gain;
+ *   d_q, d_scale = codes and scale of y;  d_resid = r.
+ *   d_x float32 [rows, d]; d_delta [rows, d] of delta_dtype (SSM_DT_F32, BF16
+ *   or F16), or NULL (r = d_x; delta_dtype is ignored); d_gain [d] of gain_dtype
+ *   (SSM_DT_F32 or BF16); d_q int8 [rows, d]; d_scale float32 [rows];
+ *   d_resid float32 [rows, d], or NULL; it may be d_x or a float32 d_delta
+ *   itself (in place) but must not overlap them otherwise.
+ * eps finite and >= 0 (with eps = 0 a row of zeros has no norm: its scale is NaN).
+ */
+int32_t ssm_norm_i8(int32_t rows, int32_t d, const float* d_x, const void* d_delta,
+                    int32_t delta_dtype, const void* d_gain, int32_t gain_dtype, float eps,
+                    float* d_resid, int8_t* d_q, float* d_scale, void* stream);
+
+/*
+ * Codes and scales of the rows of d_x [rows, d] (swiglu = 0), or of
+ * silu(gate) * up for d_x [rows, 2 d] whose rows are [gate | up] (swiglu = 1);
+ * d_x of dtype SSM_DT_F32, BF16 or F16, d_q int8 [rows, d], d_scale float32 [rows].
+ */
+int32_t ssm_quant_i8(int32_t rows, int32_t d, int32_t swiglu, int32_t dtype, const void* d_x,
+                     int8_t* d_q, float* d_scale, void* stream);
+
+/* Bytes of device workspace ssm_gemm_i8 needs for these sizes (may be 0). */
+int32_t ssm_gemm_i8_workspace_size(int32_t m, int32_t n, int32_t k, size_t* bytes);
+
+/*
+ * d_out[i, j] = d_a_scale[i] * d_w_scale[j] * sum_l d_a[i, l] * d_w[j, l]
+ * for int8 rows d_a [m, k], int8 weights d_w [n, k], float32 scales [m] and [n];
+ * d_out [m, n] of out_dtype (SSM_DT_F32, BF16 or F16).  The sums are exact
+ * int32 (any codes in [-128, 127]); the sum times the product of the two
+ * scales is computed in float32 and rounded once to out_dtype.
+ * k up to 131071 (SSM_E_UNSUPPORTED above); m = 0 launches nothing.  Rows are
+ * read fastest where k is a multiple of 16 and d_a, d_w are 16-byte aligned.
+ * d_ws: 16-byte aligned workspace of ws_bytes >= ssm_gemm_i8_workspace_size(m,
+ * n, k) (SSM_E_CAPACITY), used by one call at a time; NULL if that is 0.
+ */
+int32_t ssm_gemm_i8(int32_t m, int32_t n, int32_t k, const int8_t* d_a, const float* d_a_scale,
+                    const int8_t* d_w, const float* d_w_scale, int32_t out_dtype, void* d_out,
+                    void* d_ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Scores of tokens.                                                         */
+/* ------------------------------------------------------------------------ */
+
+/* Bytes of device workspace ssm_token_logprobs needs for these sizes (may be 0). */
+int32_t ssm_token_logprobs_workspace_size(int32_t rows, int32_t vocab, int32_t k, size_t* bytes);
+
+/*
+ * For each row of logits d_logits [rows, vocab] (dtype SSM_DT_F32, BF16 or F16:
+ * the logits of ssm_denoise_step, or those of an 8-bit head), with p the
+ * softmax over the vocabulary without mask_id (-1: nothing is left out):
+ *   d_logprob     float32 [rows, n_targets]: ln p of the tokens d_targets int32
+ *                 [rows, n_targets]; -inf for mask_id, NaN for an id outside
+ *                 [0, vocab) (padding)
+ *   d_entropy     float32 [rows] (NULL to skip): -sum p ln p, in nats
+ *   d_top_ids     int32 [rows, k]: the k most probable tokens, most probable
+ *                 first, lower id on ties; -1 past the tokens with a logit
+ *                 above -inf
+ *   d_top_logprob float32 [rows, k]: their ln p (-inf where d_top_ids is -1)
+ * A logit of -inf has probability 0 and adds nothing to the entropy.  A row
+ * with a NaN or +inf, or without any logit above -inf, has NaN log
+ * probabilities (of listed tokens) and entropy; NaN logits are not listed.
+ * k in [0, 8]; n_targets >= 0; unused outputs may be NULL (d_targets and
+ * d_logprob with n_targets = 0, the lists with k = 0).
+ * d_ws: 16-byte aligned workspace of ws_bytes >=
+ * ssm_token_logprobs_workspace_size(rows, vocab, k) (SSM_E_CAPACITY), used by
+ * one call at a time; NULL if that is 0.
+ */
+int32_t ssm_token_logprobs(int32_t rows, int32_t vocab, int32_t dtype, const void* d_logits,
+                           int32_t mask_id, int32_t n_targets, const int32_t* d_targets, int32_t k,
+                           float* d_logprob, float* d_entropy, int32_t* d_top_ids,
+                           float* d_top_logprob, void* d_ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ */
 /* Confidence-based unmasking and prediction-state update (Section 4.2).    */
 /* ------------------------------------------------------------------------ */
 
@@ -412,7 +506,8 @@ int32_t ssm_early_stop(int32_t* d_tokens, int32_t batch, int32_t seq_len, const 
  * bracketed by a pair of HIP events on the call's stream (created without
  * the system-scope fence), recorded under a tag naming the operation ("select", "embed",
  * "rope_table", "norm", "gemm_qkv", "attention", "gemm_o", "gemm_gate_up",
- * "gemm_down", "gemm_lm_head", "rowstats", "unmask", "early_stop") and the kernel's
+ * "gemm_down", "gemm_lm_head", "rowstats", "unmask", "early_stop", "norm_i8",
+ * "quant_i8", "gemm_i8", "token_logprobs") and the kernel's
  * ordinal within one call of that operation (0 = the main kernel; split-K
  * reductions and merges come after).  Each call discards earlier records.
  * Not thread-safe; meant for a single profiling thread.

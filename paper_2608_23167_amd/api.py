@@ -184,6 +184,133 @@ def ssm_gather_rows(src: torch.Tensor, pos: torch.Tensor, out: torch.Tensor, str
           "ssm_gather_rows")
 
 
+_DT = {torch.float32: L.SSM_DT_F32, torch.bfloat16: L.SSM_DT_BF16, torch.float16: L.SSM_DT_F16}
+
+
+def _dt(t: torch.Tensor, name: str) -> int:
+    code = _DT.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
+    return code
+
+
+def _shape(t: torch.Tensor, shape, name: str) -> None:
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+
+
+def _ws(ws: Optional[torch.Tensor]) -> Tuple[C.c_void_p, int]:
+    return (C.c_void_p(None), 0) if ws is None else (_ptr(ws, None, "ws"), ws.numel() * ws.element_size())
+
+
+def _on_current(*tensors: Optional[torch.Tensor]) -> None:
+    """The library launches on the current device: tensors of another are refused."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.is_cuda and t.get_device() != dev:
+            raise ValueError(f"tensors must be on the current device (cuda:{dev}), got {t.device}")
+
+
+def ssm_norm_i8(x: torch.Tensor, gain: torch.Tensor, eps: float, q: torch.Tensor,
+                scale: torch.Tensor, delta: Optional[torch.Tensor] = None,
+                resid: Optional[torch.Tensor] = None, stream=None) -> None:
+    """r = x + delta; q, scale = the int8 codes and row scales of the RMSNorm of
+    r times gain; resid (may be x) receives r.  x, resid float32 [rows, d];
+    delta [rows, d] float32, bf16 or float16; gain [d] float32 or bf16; q int8
+    [rows, d]; scale float32 [rows]."""
+    rows, d = x.shape
+    _shape(gain, (d,), "gain")
+    _shape(q, (rows, d), "q")
+    _shape(scale, (rows,), "scale")
+    if delta is not None:
+        _shape(delta, (rows, d), "delta")
+    if resid is not None:
+        _shape(resid, (rows, d), "resid")
+    args = (rows, d, _ptr(x, torch.float32, "x"), _ptr(delta, None, "delta"),
+            0 if delta is None else _dt(delta, "delta"), _ptr(gain, None, "gain"),
+            _dt(gain, "gain"), float(eps), _ptr(resid, torch.float32, "resid"),
+            _ptr(q, torch.int8, "q"), _ptr(scale, torch.float32, "scale"))
+    _on_current(x, gain, q, scale, delta, resid)
+    check(lib().ssm_norm_i8(*args, _stream(stream)), "ssm_norm_i8")
+
+
+def ssm_quant_i8(x: torch.Tensor, q: torch.Tensor, scale: torch.Tensor, swiglu: bool = False,
+                 stream=None) -> None:
+    """q, scale = the int8 codes and row scales of x [rows, d], or with swiglu of
+    silu(x[:, :d]) * x[:, d:] for x [rows, 2 d]; x float32, bf16 or float16; q
+    int8 [rows, d]; scale float32 [rows]."""
+    rows, d = q.shape
+    _shape(x, (rows, 2 * d if swiglu else d), "x")
+    _shape(scale, (rows,), "scale")
+    args = (rows, d, int(bool(swiglu)), _dt(x, "x"), _ptr(x, None, "x"), _ptr(q, torch.int8, "q"),
+            _ptr(scale, torch.float32, "scale"))
+    _on_current(x, q, scale)
+    check(lib().ssm_quant_i8(*args, _stream(stream)), "ssm_quant_i8")
+
+
+def ssm_gemm_i8_workspace_size(m: int, n: int, k: int) -> int:
+    b = C.c_size_t()
+    check(lib().ssm_gemm_i8_workspace_size(m, n, k, C.byref(b)), "ssm_gemm_i8_workspace_size")
+    return b.value
+
+
+def ssm_gemm_i8(a: torch.Tensor, a_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor,
+                out: torch.Tensor, ws: Optional[torch.Tensor], stream=None) -> None:
+    """out[m, n] = a_scale[m] * w_scale[n] * sum_k a[m, k] * w[n, k]; a int8 [M, K],
+    w int8 [N, K], scales float32 [M] and [N], out [M, N] float32, bf16 or
+    float16; ws uint8 of ssm_gemm_i8_workspace_size(M, N, K) bytes (None if 0)."""
+    (m, k), n = a.shape, w.shape[0]
+    _shape(w, (n, k), "w")
+    _shape(a_scale, (m,), "a_scale")
+    _shape(w_scale, (n,), "w_scale")
+    _shape(out, (m, n), "out")
+    args = (m, n, k, _ptr(a, torch.int8, "a"), _ptr(a_scale, torch.float32, "a_scale"),
+            _ptr(w, torch.int8, "w"), _ptr(w_scale, torch.float32, "w_scale"), _dt(out, "out"),
+            _ptr(out, None, "out"), *_ws(ws))
+    _on_current(a, a_scale, w, w_scale, out, ws)
+    check(lib().ssm_gemm_i8(*args, _stream(stream)), "ssm_gemm_i8")
+
+
+def ssm_token_logprobs_workspace_size(rows: int, vocab: int, k: int) -> int:
+    b = C.c_size_t()
+    check(lib().ssm_token_logprobs_workspace_size(rows, vocab, k, C.byref(b)),
+          "ssm_token_logprobs_workspace_size")
+    return b.value
+
+
+def ssm_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor], mask_id: int, k: int,
+                       logprob: Optional[torch.Tensor], entropy: Optional[torch.Tensor],
+                       top_ids: Optional[torch.Tensor], top_logprob: Optional[torch.Tensor],
+                       ws: Optional[torch.Tensor], stream=None) -> None:
+    """Scores of logits [rows, vocab] (float32, bf16 or float16) with the token
+    mask_id left out (-1: none): logprob float32 [rows, T] of targets int32
+    [rows, T] (both None: no targets), entropy float32 [rows] (None to skip),
+    the k most probable tokens top_ids int32 and top_logprob float32 [rows, k]
+    (both None with k = 0); ws uint8 of ssm_token_logprobs_workspace_size(rows,
+    vocab, k) bytes (None if 0)."""
+    rows, vocab = logits.shape
+    if (targets is None) != (logprob is None):
+        raise ValueError("targets and logprob go together")
+    t = 0
+    if targets is not None:
+        t = targets.shape[1]
+        _shape(targets, (rows, t), "targets")
+        _shape(logprob, (rows, t), "logprob")
+    if entropy is not None:
+        _shape(entropy, (rows,), "entropy")
+    if k > 0:
+        if top_ids is None or top_logprob is None:
+            raise ValueError("k > 0 needs top_ids and top_logprob")
+        _shape(top_ids, (rows, k), "top_ids")
+        _shape(top_logprob, (rows, k), "top_logprob")
+    args = (rows, vocab, _dt(logits, "logits"), _ptr(logits, None, "logits"), int(mask_id), t,
+            _ptr(targets, torch.int32, "targets"), int(k), _ptr(logprob, torch.float32, "logprob"),
+            _ptr(entropy, torch.float32, "entropy"), _ptr(top_ids, torch.int32, "top_ids"),
+            _ptr(top_logprob, torch.float32, "top_logprob"), *_ws(ws))
+    _on_current(logits, targets, logprob, entropy, top_ids, top_logprob, ws)
+    check(lib().ssm_token_logprobs(*args, _stream(stream)), "ssm_token_logprobs")
+
+
 def ssm_unmask(tokens: torch.Tensor, block_start: int, block_size: int, mask_id: int, rule: int,
                n_per_step: int, threshold: float, argmax: torch.Tensor, conf: torch.Tensor,
                topk_ids: torch.Tensor, topk_w: torch.Tensor, k: int, n_out: int,
@@ -217,7 +344,8 @@ def ssm_early_stop(tokens: torch.Tensor, block_start: int, block_size: int, eos_
 
 
 PROFILE_TAGS = ("select", "embed", "rope_table", "norm", "gemm_qkv", "attention", "gemm_o",
-                "gemm_gate_up", "gemm_down", "gemm_lm_head", "rowstats", "unmask", "early_stop")
+                "gemm_gate_up", "gemm_down", "gemm_lm_head", "rowstats", "unmask", "early_stop",
+                "norm_i8", "quant_i8", "gemm_i8", "token_logprobs")
 
 
 def ssm_profile_enable(on: bool) -> None:

@@ -581,6 +581,110 @@ int32_t ssm_gather_rows(int32_t batch, int32_t src_rows, int32_t width, const vo
   return ok();
 }
 
+// Element types of the 8-bit projections' inputs and outputs.
+static bool float_dtype(int32_t dt) { return dt == SSM_DT_F32 || dt == SSM_DT_BF16 || dt == SSM_DT_F16; }
+
+// Rows are dealt out one workgroup each, so their number is a grid size.
+static constexpr int32_t I8_MAX_ROWS = 1 << 24;
+// Sums of K products of codes in [-128, 127] stay below 2^31.
+static constexpr int32_t I8_MAX_K = (1 << 17) - 1;
+
+int32_t ssm_norm_i8(int32_t rows, int32_t d, const float* d_x, const void* d_delta,
+                    int32_t delta_dtype, const void* d_gain, int32_t gain_dtype, float eps,
+                    float* d_resid, int8_t* d_q, float* d_scale, void* stream) {
+  if (rows < 0 || rows > I8_MAX_ROWS || d < 1) return fail(SSM_E_INVAL, "bad sizes (rows %d, d %d)", rows, d);
+  if (d_delta && !float_dtype(delta_dtype)) return fail(SSM_E_INVAL, "unknown delta_dtype %d", delta_dtype);
+  if (gain_dtype != SSM_DT_F32 && gain_dtype != SSM_DT_BF16)
+    return fail(SSM_E_INVAL, "gain_dtype must be SSM_DT_F32 or SSM_DT_BF16 (got %d)", gain_dtype);
+  if (!(eps >= 0.f) || eps > 3.4e38f) return fail(SSM_E_INVAL, "eps must be finite and not negative");
+  if (rows > 0 && (!d_x || !d_gain || !d_q || !d_scale)) return fail(SSM_E_INVAL, "null device pointer");
+  hipStream_t st = (hipStream_t)stream;
+  PROF_TRY("norm_i8", launch_norm_i8(rows, d, d_x, d_delta, delta_dtype, d_gain, gain_dtype, eps,
+                                     d_resid, d_q, d_scale, st));
+  return ok();
+}
+
+int32_t ssm_quant_i8(int32_t rows, int32_t d, int32_t swiglu, int32_t dtype, const void* d_x,
+                     int8_t* d_q, float* d_scale, void* stream) {
+  if (rows < 0 || rows > I8_MAX_ROWS || d < 1 || d > (1 << 30))
+    return fail(SSM_E_INVAL, "bad sizes (rows %d, d %d)", rows, d);
+  if (swiglu != 0 && swiglu != 1) return fail(SSM_E_INVAL, "swiglu must be 0 or 1 (got %d)", swiglu);
+  if (!float_dtype(dtype)) return fail(SSM_E_INVAL, "unknown dtype %d", dtype);
+  if (rows > 0 && (!d_x || !d_q || !d_scale)) return fail(SSM_E_INVAL, "null device pointer");
+  hipStream_t st = (hipStream_t)stream;
+  PROF_TRY("quant_i8", launch_quant_i8(dtype, rows, d, swiglu != 0, d_x, d_q, d_scale, st));
+  return ok();
+}
+
+static int32_t check_gemm_i8(int32_t m, int32_t n, int32_t k) {
+  if (m < 0 || m > I8_MAX_ROWS || n < 1 || n > I8_MAX_ROWS || k < 1)
+    return fail(SSM_E_INVAL, "bad sizes (m %d, n %d, k %d)", m, n, k);
+  if (k > I8_MAX_K) return fail(SSM_E_UNSUPPORTED, "k %d above %d: an int32 sum could overflow", k, I8_MAX_K);
+  // the grid of the kernel for any alignment has ceil(m / 64) workgroups in y
+  if (m > 64 * 65535) return fail(SSM_E_UNSUPPORTED, "m %d above %d rows", m, 64 * 65535);
+  return SSM_OK;
+}
+
+int32_t ssm_gemm_i8_workspace_size(int32_t m, int32_t n, int32_t k, size_t* bytes) {
+  if (!bytes) return fail(SSM_E_INVAL, "null argument");
+  int32_t rc = check_gemm_i8(m, n, k);
+  if (rc) return rc;
+  *bytes = gemm_i8_ws_bytes(m, n, k);
+  return ok();
+}
+
+int32_t ssm_gemm_i8(int32_t m, int32_t n, int32_t k, const int8_t* d_a, const float* d_a_scale,
+                    const int8_t* d_w, const float* d_w_scale, int32_t out_dtype, void* d_out,
+                    void* d_ws, size_t ws_bytes, void* stream) {
+  int32_t rc = check_gemm_i8(m, n, k);
+  if (rc) return rc;
+  if (!float_dtype(out_dtype)) return fail(SSM_E_INVAL, "unknown out_dtype %d", out_dtype);
+  if (m > 0 && (!d_a || !d_a_scale || !d_w || !d_w_scale || !d_out)) return fail(SSM_E_INVAL, "null device pointer");
+  const size_t need = gemm_i8_ws_bytes(m, n, k);
+  if (ws_bytes < need) return fail(SSM_E_CAPACITY, "workspace %zu < %zu bytes", ws_bytes, need);
+  if (need > 0 && (!d_ws || ((uintptr_t)d_ws & 15))) return fail(SSM_E_INVAL, "workspace null or not 16-byte aligned");
+  hipStream_t st = (hipStream_t)stream;
+  PROF_TRY("gemm_i8", gemm_i8(m, n, k, d_a, d_a_scale, d_w, d_w_scale, out_dtype, d_out, d_ws, st));
+  return ok();
+}
+
+static int32_t check_logprobs(int32_t rows, int32_t vocab, int32_t k) {
+  if (rows < 0 || rows > I8_MAX_ROWS || vocab < 1 || vocab > (1 << 30))
+    return fail(SSM_E_INVAL, "bad sizes (rows %d, vocab %d)", rows, vocab);
+  if (k < 0 || k > 8) return fail(SSM_E_INVAL, "k %d not in [0, 8]", k);
+  return SSM_OK;
+}
+
+int32_t ssm_token_logprobs_workspace_size(int32_t rows, int32_t vocab, int32_t k, size_t* bytes) {
+  if (!bytes) return fail(SSM_E_INVAL, "null argument");
+  int32_t rc = check_logprobs(rows, vocab, k);
+  if (rc) return rc;
+  *bytes = token_logprobs_ws_bytes(rows, vocab, k);
+  return ok();
+}
+
+int32_t ssm_token_logprobs(int32_t rows, int32_t vocab, int32_t dtype, const void* d_logits,
+                           int32_t mask_id, int32_t n_targets, const int32_t* d_targets, int32_t k,
+                           float* d_logprob, float* d_entropy, int32_t* d_top_ids,
+                           float* d_top_logprob, void* d_ws, size_t ws_bytes, void* stream) {
+  int32_t rc = check_logprobs(rows, vocab, k);
+  if (rc) return rc;
+  if (!float_dtype(dtype)) return fail(SSM_E_INVAL, "unknown dtype %d", dtype);
+  if (mask_id < -1 || mask_id >= vocab) return fail(SSM_E_INVAL, "mask_id %d not in [-1, vocab)", mask_id);
+  if (n_targets < 0) return fail(SSM_E_INVAL, "n_targets %d < 0", n_targets);
+  if (rows > 0 && (!d_logits || (n_targets > 0 && (!d_targets || !d_logprob)) ||
+                   (k > 0 && (!d_top_ids || !d_top_logprob))))
+    return fail(SSM_E_INVAL, "null device pointer");
+  const size_t need = token_logprobs_ws_bytes(rows, vocab, k);
+  if (ws_bytes < need) return fail(SSM_E_CAPACITY, "workspace %zu < %zu bytes", ws_bytes, need);
+  if (need > 0 && (!d_ws || ((uintptr_t)d_ws & 15))) return fail(SSM_E_INVAL, "workspace null or not 16-byte aligned");
+  hipStream_t st = (hipStream_t)stream;
+  PROF_TRY("token_logprobs", launch_token_logprobs(dtype, rows, vocab, d_logits, mask_id, n_targets,
+                                                   d_targets, k, d_logprob, d_entropy, d_top_ids,
+                                                   d_top_logprob, d_ws, st));
+  return ok();
+}
+
 int32_t ssm_unmask(int32_t* d_tokens, int32_t batch, int32_t seq_len, const int32_t* pad,
                    int32_t block_start, int32_t block_size, int32_t mask_id, int32_t rule,
                    int32_t n_per_step, float threshold, const int32_t* d_argmax, const float* d_conf,

@@ -274,6 +274,29 @@ hipError_t attention(int dtype, const void* q, const void* kc, const void* vc, i
                      int Hkv, int dh, int Mq, int Nk, int cap, const ActOut& out, AttnWs ws,
                      const Pads& pads, hipStream_t st);
 
+// ---- 8-bit projections ------------------------------------------------------
+// dtype codes: 0 float32, 1 bfloat16, 2 float16 (gains: 0 or 1).
+// r = x (+ delta); codes and scale of g r / sqrt(mean(r^2) + eps); resid (may be
+// null, may be x) receives r.
+hipError_t launch_norm_i8(int rows, int d, const float* x, const void* delta, int delta_dtype,
+                          const void* g, int gain_dtype, float eps, float* resid, int8_t* q,
+                          float* scale, hipStream_t st);
+// Codes and scales of the rows of x [rows, d], or of silu(gate) * up for
+// x [rows, 2 d] = [gate | up].
+hipError_t launch_quant_i8(int dtype, int rows, int d, bool swiglu, const void* x, int8_t* q,
+                           float* scale, hipStream_t st);
+// out[m, n] = sa[m] * sw[n] * sum_k a[m, k] w[n, k].
+size_t gemm_i8_ws_bytes(int M, int N, int K);
+hipError_t gemm_i8(int M, int N, int K, const int8_t* a, const float* sa, const int8_t* w,
+                   const float* sw, int out_dtype, void* out, void* ws, hipStream_t st);
+
+// ---- scores of tokens ---------------------------------------------------------
+size_t token_logprobs_ws_bytes(int rows, int V, int k);
+hipError_t launch_token_logprobs(int dtype, int rows, int V, const void* logits, int mask_id,
+                                 int n_targets, const int32_t* targets, int k, float* lp,
+                                 float* entropy, int32_t* top_ids, float* top_lp, void* ws,
+                                 hipStream_t st);
+
 // ---- unmasking ------------------------------------------------------------
 hipError_t launch_unmask(int32_t* tokens, int batch, int seq_len, int block_start, int b,
                          int mask_id, int rule, int n_per_step, float threshold,
