@@ -46,11 +46,156 @@ __device__ __forceinline__ int8_t code(float y, float inv) {
   return inv == 0.f ? (int8_t)0 : (int8_t)__float2int_rn(y * inv);
 }
 
+__device__ __forceinline__ float swiglu(float g, float u) { return g / (1.f + expf(-g)) * u; }
+
+// ---- rows held in registers ---------------------------------------------------
+// TPR threads to a row (64: four rows to a workgroup, each a wave of its own;
+// 256 or 1024: the workgroup), NV pieces of V elements to a thread, piece
+// number t + TPR i of the row.  Every element is read once, the row's sum and
+// largest magnitude are reduced together, and the codes leave from registers.
+template <int V, typename T> __device__ __forceinline__ void load_v(const T* p, float (&v)[V]) {
+  if constexpr (V == 1) {
+    v[0] = ldf(p);
+  } else if constexpr (std::is_same<T, float>::value) {
+    const float4 f = *(const float4*)p;
+    v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
+  } else {
+    const uint2 u = *(const uint2*)p;
+    const T* e = (const T*)&u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = ldf(e + i);
+  }
+}
+template <int V> __device__ __forceinline__ void store_codes(int8_t* q, const float (&y)[V], float inv) {
+  if constexpr (V == 1) {
+    *q = code(y[0], inv);
+  } else {
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w |= (uint32_t)(uint8_t)code(y[i], inv) << (8 * i);
+    *(uint32_t*)q = w;
+  }
+}
+
+// Sum and largest bits over the TPR threads of a row.
+template <int TPR>
+__device__ __forceinline__ void row_reduce(float& s, uint32_t& a, float* red, uint32_t* redu) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    s += __shfl_xor(s, o, 64);
+    a = max(a, (uint32_t)__shfl_xor((int)a, o, 64));
+  }
+  if constexpr (TPR > 64) {
+    if ((threadIdx.x & 63) == 0) { red[threadIdx.x >> 6] = s; redu[threadIdx.x >> 6] = a; }
+    __syncthreads();
+    s = 0.f;
+#pragma unroll
+    for (int w = 0; w < TPR / 64; ++w) { s += red[w]; a = max(a, redu[w]); }
+  }
+}
+
+template <typename T, bool SWIGLU, int V, int NV, int TPR>
+__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR)
+quant_rows_kernel(const T* __restrict__ x, int rows, int d, int8_t* __restrict__ q,
+                  float* __restrict__ scale) {
+  constexpr int RPB = TPR < 256 ? 256 / TPR : 1;
+  __shared__ float red[16];
+  __shared__ uint32_t redu[16];
+  const int t = threadIdx.x % TPR;
+  const size_t row = (size_t)blockIdx.x * RPB + threadIdx.x / TPR;
+  if (row >= (size_t)rows) return;                  // whole waves, and only where a wave is a row
+  const T* xr = x + row * d * (SWIGLU ? 2 : 1);
+  float y[NV][V];
+  uint32_t a = 0;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = (t + TPR * i) * V;
+    if (c < d) {
+      load_v<V>(xr + c, y[i]);
+      if constexpr (SWIGLU) {
+        float u[V];
+        load_v<V>(xr + d + c, u);
+#pragma unroll
+        for (int e = 0; e < V; ++e) y[i][e] = swiglu(y[i][e], u[e]);
+      }
+#pragma unroll
+      for (int e = 0; e < V; ++e) a = max(a, abs_bits(y[i][e]));
+    }
+  }
+  float none = 0.f;
+  row_reduce<TPR>(none, a, red, redu);
+  const Codes k = codes_of(a);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = (t + TPR * i) * V;
+    if (c < d) store_codes<V>(q + row * d + c, y[i], k.inv);
+  }
+  if (t == 0) scale[row] = k.scale;
+}
+
+// The largest |y| is the largest |r g| times 1 / rms, so one reduction serves
+// both statistics.  resid may be x or delta: a thread reads its elements first.
+template <typename TD, typename TG, int V, int NV, int TPR>
+__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR)
+norm_rows_kernel(const float* x, const TD* delta, const TG* __restrict__ g, int rows, int d, float eps,
+                 float* resid, int8_t* __restrict__ q, float* __restrict__ scale) {
+  constexpr int RPB = TPR < 256 ? 256 / TPR : 1;
+  __shared__ float red[16];
+  __shared__ uint32_t redu[16];
+  const int t = threadIdx.x % TPR;
+  const size_t row = (size_t)blockIdx.x * RPB + threadIdx.x / TPR;
+  if (row >= (size_t)rows) return;
+  const size_t at = row * d;
+  float r[NV][V], dv[NV][V], gv[NV][V];             // all loads first: one trip to memory
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = (t + TPR * i) * V;
+    if (c < d) {
+      load_v<V>(x + at + c, r[i]);
+      if (delta) load_v<V>(delta + at + c, dv[i]);
+      load_v<V>(g + c, gv[i]);
+    }
+  }
+  float ss = 0.f;
+  uint32_t a = 0;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = (t + TPR * i) * V;
+    if (c < d) {
+      if (delta) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) r[i][e] += dv[i][e];
+      }
+      if (resid) {
+        if constexpr (V == 4) *(float4*)(resid + at + c) = make_float4(r[i][0], r[i][1], r[i][2], r[i][3]);
+        else resid[at + c] = r[i][0];
+      }
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        ss += r[i][e] * r[i][e];
+        r[i][e] *= gv[i][e];
+        a = max(a, abs_bits(r[i][e]));
+      }
+    }
+  }
+  row_reduce<TPR>(ss, a, red, redu);
+  const float inv = 1.0f / sqrtf(ss / (float)d + eps);
+  const Codes k = codes_of(abs_bits(__uint_as_float(a) * inv));
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = (t + TPR * i) * V;
+#pragma unroll
+    for (int e = 0; e < V; ++e) r[i][e] *= inv;
+    if (c < d) store_codes<V>(q + at + c, r[i], k.inv);
+  }
+  if (t == 0) scale[row] = k.scale;
+}
+
+// ---- rows of any width, read again in each pass -----------------------------------
 template <typename T> struct RowValue {           // plain rows
   const T* x;
   __device__ __forceinline__ float operator()(int c) const { return ldf(x + c); }
 };
-__device__ __forceinline__ float swiglu(float g, float u) { return g / (1.f + expf(-g)) * u; }
 template <typename T> struct SwigluValue {        // gate in [0, d), up in [d, 2 d)
   const T* x;
   int d;
@@ -101,8 +246,38 @@ __global__ void __launch_bounds__(256) norm_i8_kernel(const float* x, const TD* 
   if (threadIdx.x == 0) scale[blockIdx.x] = k.scale;
 }
 
+static bool aligned(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
+
+// The register form for a row of d elements, in pieces of 4 where the addresses
+// allow it: the fewest threads that hold the row.
+#define ROWS_DISPATCH(GO)                 \
+  do {                                    \
+    if (vec) {                            \
+      if (d <= 1024) GO(4, 4, 64);        \
+      if (d <= 4096) GO(4, 4, 256);       \
+      if (d <= 8192) GO(4, 8, 256);       \
+      if (d <= 16384) GO(4, 4, 1024);     \
+      if (d <= 32768) GO(4, 8, 1024);     \
+    } else {                              \
+      if (d <= 1024) GO(1, 16, 64);       \
+      if (d <= 4096) GO(1, 16, 256);      \
+      if (d <= 8192) GO(1, 32, 256);      \
+      if (d <= 32768) GO(1, 32, 1024);    \
+    }                                     \
+  } while (0)
+
 template <typename T>
 static hipError_t quant_t(int rows, int d, bool sw, const T* x, int8_t* q, float* scale, hipStream_t st) {
+  const bool vec = d % 4 == 0 && aligned(x, 4 * sizeof(T)) && aligned(q, 4);
+#define QUANT(V, NV, TPR)                                                                            \
+  do {                                                                                               \
+    const dim3 grid(ceil_div(rows, TPR < 256 ? 256 / TPR : 1)), block(TPR < 256 ? 256 : TPR);        \
+    if (sw) launch((quant_rows_kernel<T, true, V, NV, TPR>), grid, block, 0, st, x, rows, d, q, scale); \
+    else launch((quant_rows_kernel<T, false, V, NV, TPR>), grid, block, 0, st, x, rows, d, q, scale);   \
+    return hipGetLastError();                                                                        \
+  } while (0)
+  ROWS_DISPATCH(QUANT);
+#undef QUANT
   if (sw) launch(quant_i8_kernel<T, true>, dim3(rows), dim3(256), 0, st, x, d, q, scale);
   else launch(quant_i8_kernel<T, false>, dim3(rows), dim3(256), 0, st, x, d, q, scale);
   return hipGetLastError();
@@ -119,6 +294,16 @@ hipError_t launch_quant_i8(int dtype, int rows, int d, bool swiglu, const void* 
 template <typename TD, typename TG>
 static hipError_t norm_t(int rows, int d, const float* x, const TD* delta, const TG* g, float eps,
                          float* resid, int8_t* q, float* scale, hipStream_t st) {
+  const bool vec = d % 4 == 0 && aligned(x, 16) && aligned(g, 4 * sizeof(TG)) && aligned(q, 4) &&
+                   aligned(delta, 4 * sizeof(TD)) && aligned(resid, 16);
+#define NORM(V, NV, TPR)                                                                        \
+  do {                                                                                          \
+    launch((norm_rows_kernel<TD, TG, V, NV, TPR>), dim3(ceil_div(rows, TPR < 256 ? 256 / TPR : 1)), \
+           dim3(TPR < 256 ? 256 : TPR), 0, st, x, delta, g, rows, d, eps, resid, q, scale);     \
+    return hipGetLastError();                                                                   \
+  } while (0)
+  ROWS_DISPATCH(NORM);
+#undef NORM
   launch(norm_i8_kernel<TD, TG>, dim3(rows), dim3(256), 0, st, x, delta, g, d, eps, resid, q, scale);
   return hipGetLastError();
 }

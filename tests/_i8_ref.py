@@ -58,9 +58,10 @@ def norm(r, gain, eps):
 
 
 def norm_rel(d):
-    """Squares summed in 256 chains of d / 256 and 10 more additions, halved by
-    the square root; mean, eps, root, inverse and two products after it."""
-    return (d / 512 + 12) * U
+    """Squares summed in chains of at most max(16, d / 256), and 16 more additions
+    to join them; halved by the square root; mean, eps, root, inverse and two
+    products after it."""
+    return ((max(16, d / 256) + 16) / 2 + 6) * U
 
 
 SWIGLU_REL = 12 * U      # an exponential, an addition, a division, a product; the sum's own size
