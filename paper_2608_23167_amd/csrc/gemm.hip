@@ -43,6 +43,7 @@
 
 #include "internal.h"
 #include "row_stats.h"
+#include "tiles.h"
 
 namespace ssm {
 
@@ -409,23 +410,6 @@ __device__ __forceinline__ void tile_epilogue(const Pol& pol, const float* Cs, i
 // ---------------------------------------------------------------------------
 // bfloat16 MFMA kernel
 // ---------------------------------------------------------------------------
-// Tile order: the grid is 1-D over (split, n-tile, m-tile) triples.
-// Workgroups are dealt to the 8 XCDs round-robin by linear id, so id w runs
-// on XCD w % 8; the order below gives each XCD a contiguous range of the
-// triples, split-major, then n-tiles, m-tiles innermost.  The workgroups that
-// share a weight tile then run on the same XCD at about the same time and
-// read it once into that XCD's L2, and each XCD touches as few K-slices of
-// the activations as possible, so that its slice stays resident in its L2.
-__device__ __forceinline__ void tile_of(int w, int total, int ntm, int mt, int& split, int& tn,
-                                        int& tm) {
-  const int per = total / 8;
-  const int v = w < per * 8 ? (w % 8) * per + (w / 8) : w;
-  split = v / ntm;
-  const int t = v % ntm;
-  tn = t / mt;
-  tm = t % mt;
-}
-
 // K-step handover between the two kinds of waves.  The buffer schedule below
 // never lets a compute wave read an LDS buffer in the step in which it is
 // rewritten, so the compute waves pass the barrier without waiting for their
@@ -658,13 +642,6 @@ __global__ void __launch_bounds__(512) gemm_bf16_kernel(Pol pol, const bf16_t* _
   }
 }
 
-// Waits until at most N vector-memory operations of this wave are in flight.
-template <int N>
-__device__ __forceinline__ void wait_vmcnt() {
-  static_assert(N >= 0 && N < 64, "vmcnt range");
-  __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (15 << 8) | ((N >> 4) << 14));
-}
-
 // ---------------------------------------------------------------------------
 // bfloat16 MFMA kernel, two wave groups in alternation
 // ---------------------------------------------------------------------------
@@ -699,12 +676,6 @@ __device__ __forceinline__ void wait_vmcnt() {
 // different 16-byte columns of the banks.
 // The MFMA takes the weights as its first operand: a lane then holds 4
 // consecutive columns of one row, and the epilogue runs from registers.
-__device__ __forceinline__ void pp_barrier() {
-  __builtin_amdgcn_sched_barrier(0);
-  asm volatile("s_barrier" ::: "memory");
-  __builtin_amdgcn_sched_barrier(0);
-}
-
 template <int BM, int BN, int WM, int WN, bool SPLIT, class Pol>
 __global__ void __launch_bounds__(512, 2) gemm_pp_kernel(Pol pol, const bf16_t* __restrict__ Ahi,
                                                            const bf16_t* __restrict__ Alo, int G,
