@@ -5,135 +5,305 @@
 //   log p(v) = (x_v - m) - ln z,   entropy = ln z - t / z.
 // (m, z, t) of two parts join by moving both to the larger maximum M: for
 // delta = m - M, z -> z e^delta and t -> e^delta (t + z delta).
-// Logits of -inf (and the [MASK] id, which counts as one) add nothing; a row
-// with a NaN or a +inf has NaN log probabilities and entropy.
+// Logits of -inf (and the [MASK] id, which counts as one) add nothing.  A row
+// with a NaN or a +inf, or with nothing above -inf, has an m that is not
+// finite, and m - m makes its log probabilities and entropy NaN.
 #include "internal.h"
 #include "row_stats.h"
 
 namespace ssm {
 
+constexpr float LOG2E = 1.44269504088896340736f;
+
+// The larger of two, NaN if either is (fmaxf drops it).
+__device__ __forceinline__ float max_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+// e^y for y <= 0, as v_exp_f32 gives it (one unit in the last place; y log2(e) is
+// rounded, which is |y| half units more).
+__device__ __forceinline__ float exp_neg(float y) { return __builtin_amdgcn_exp2f(y * LOG2E); }
+
 struct Soft {
   float m, z, t;
 };
-__device__ __forceinline__ Soft soft_empty() { return {-INFINITY, 0.f, 0.f}; }
-// Differences to a maximum, no lower than SOFT_LOW: its exponential is 0 in
+// A difference to a maximum, no lower than SOFT_LOW: its exponential is 0 in
 // float32, and products with a finite number stay finite (0 * -inf is NaN).
-// NaN stays NaN.
+// The NaN of -inf - -inf becomes SOFT_LOW too; that of a NaN logit lives on in m.
 constexpr float SOFT_LOW = -200.f;
-__device__ __forceinline__ float soft_diff(float x, float m) {
-  const float y = x - m;
-  return y < SOFT_LOW ? SOFT_LOW : y;
-}
+__device__ __forceinline__ float soft_diff(float x, float m) { return fmaxf(x - m, SOFT_LOW); }
 __device__ __forceinline__ void soft_move(Soft& a, float m) {     // to the maximum m >= a.m
-  const float dl = soft_diff(a.m, m), e = expf(dl);
+  const float dl = soft_diff(a.m, m), e = exp_neg(dl);
   a.t = e * (a.t + a.z * dl);
   a.z *= e;
   a.m = m;
 }
-__device__ __forceinline__ void soft_add(Soft& a, float x) {
-  if (x == -INFINITY) return;
-  if (x > a.m) soft_move(a, x);
-  const float y = soft_diff(x, a.m), e = expf(y);
-  a.z += e;
-  a.t += e * y;
-}
 __device__ __forceinline__ Soft soft_join(Soft a, Soft b) {
-  if (b.z == 0.f) return a;
-  if (a.z == 0.f) return b;
-  const float M = fmaxf(a.m, b.m);
-  if (M > a.m) soft_move(a, M);
-  if (M > b.m) soft_move(b, M);
+  const float M = max_nan(a.m, b.m);
+  soft_move(a, M);
+  soft_move(b, M);
   return {M, a.z + b.z, a.t + b.t};
 }
+// Over the lanes of a wave, in the same order in every lane.
 __device__ __forceinline__ Soft soft_wave(Soft a) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
     const Soft b{__shfl_xor(a.m, o, 64), __shfl_xor(a.z, o, 64), __shfl_xor(a.t, o, 64)};
-    a = (threadIdx.x & o) ? soft_join(b, a) : soft_join(a, b);   // the same order in every lane
+    a = (threadIdx.x & o) ? soft_join(b, a) : soft_join(a, b);
   }
   return a;
 }
+__device__ __forceinline__ float lane_of(float v, int lane) {
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
+}
 
-// One workgroup of 256 threads per row.
-template <typename T>
-__global__ void __launch_bounds__(256) logprobs_kernel(const T* __restrict__ logits, int V,
-                                                       int mask_id, int n_targets,
-                                                       const int32_t* __restrict__ targets, int k,
-                                                       float* __restrict__ lp,
-                                                       float* __restrict__ entropy,
-                                                       int32_t* __restrict__ top_ids,
-                                                       float* __restrict__ top_lp) {
-  __shared__ Soft part[4];
-  __shared__ float bv[4];
-  __shared__ int bi[4];
-  const size_t row = blockIdx.x;
-  const int tid = threadIdx.x, wave = tid >> 6;
-  const T* L = logits + row * V;
-  float lv[STAT_K];
-  int li[STAT_K];
-#pragma unroll
-  for (int q = 0; q < STAT_K; ++q) { lv[q] = -INFINITY; li[q] = STAT_NONE; }
-  Soft a = soft_empty();
-  for (int v = tid; v < V; v += 256) {
-    if (v == mask_id) continue;
-    const float x = ldf(L + v);
-    soft_add(a, x);
-    if (x > lv[STAT_K - 1]) stat_insert(lv, li, x, v);
-  }
-  a = soft_wave(a);
-  if ((tid & 63) == 0) part[wave] = a;
-  __syncthreads();
-  a = soft_join(soft_join(part[0], part[1]), soft_join(part[2], part[3]));
-  const float lz = logf(a.z);
-  if (tid == 0 && entropy) entropy[row] = lz - a.t / a.z;
-  for (int i = tid; i < n_targets; i += 256) {
-    const int id = targets[row * n_targets + i];
-    float r = __uint_as_float(0x7fc00000u);
-    if (id >= 0 && id < V) r = ((id == mask_id ? -INFINITY : ldf(L + id)) - a.m) - lz;
-    lp[row * n_targets + i] = r;
-  }
-  for (int q = 0; q < k; ++q) {                     // the best of the threads' best, k times
-    float v = lv[0];
-    int i = li[0];
+// The k best of up to 64 lists, best first, list l in lane l: next(j) gives entry
+// j < k of this lane's list (value -inf and id STAT_NONE past its end), and
+// emit(q, v, i) gets the q-th best in every lane.
+template <class Next, class Emit>
+__device__ __forceinline__ void merge_lists(int k, Next next, Emit emit) {
+  float v;
+  int i, at = 0;
+  next(0, v, i);
+  for (int q = 0; q < k; ++q) {
+    float bv = v;
+    int bi = i;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) {
-      const float ov = __shfl_xor(v, o, 64);
-      const int oi = __shfl_xor(i, o, 64);
-      if (stat_better(ov, oi, v, i)) { v = ov; i = oi; }
+      const float ov = __shfl_xor(bv, o, 64);
+      const int oi = __shfl_xor(bi, o, 64);
+      if (stat_better(ov, oi, bv, bi)) { bv = ov; bi = oi; }
     }
-    __syncthreads();
-    if ((tid & 63) == 0) { bv[wave] = v; bi[wave] = i; }
-    __syncthreads();
-    for (int w = 0; w < 4; ++w)
-      if (stat_better(bv[w], bi[w], v, i)) { v = bv[w]; i = bi[w]; }
-    if (tid == 0) {
-      top_ids[row * k + q] = i == STAT_NONE ? -1 : i;
-      top_lp[row * k + q] = i == STAT_NONE ? -INFINITY : (v - a.m) - lz;
-    }
-    if (li[0] == i && i != STAT_NONE) {
-#pragma unroll
-      for (int u = 0; u + 1 < STAT_K; ++u) { lv[u] = lv[u + 1]; li[u] = li[u + 1]; }
-      lv[STAT_K - 1] = -INFINITY;
-      li[STAT_K - 1] = STAT_NONE;
+    emit(q, bv, bi);
+    if (i == bi && bi != STAT_NONE) {              // ids are different: one lane's
+      if (++at < k) next(at, v, i);
+      else { v = -INFINITY; i = STAT_NONE; }
     }
   }
 }
 
+// Statistics of one part of a row, as the second launch reads them.
+struct Part {
+  Soft s;
+  float v[STAT_K];
+  int id[STAT_K];
+};
+
+// Results of a row from its statistics: every lane of a wave calls it, next as in
+// merge_lists.
+template <typename T, class Next>
+__device__ __forceinline__ void row_results(size_t row, const Soft& s, const T* L, int V, int mask_id,
+                                            int n_targets, const int32_t* targets, int k, float* lp,
+                                            float* entropy, int32_t* top_ids, float* top_lp, Next next) {
+  const int lane = threadIdx.x & 63;
+  const float spoilt = s.m - s.m;                  // 0, or NaN
+  const float lz = logf(s.z);
+  if (lane == 0 && entropy) entropy[row] = (lz - s.t / s.z) + spoilt;
+  for (int i = lane; i < n_targets; i += 64) {
+    const int id = targets[row * n_targets + i];
+    float r = __uint_as_float(0x7fc00000u);
+    if (id >= 0 && id < V) r = (((id == mask_id ? -INFINITY : ldf(L + id)) - s.m) - lz) + spoilt;
+    lp[row * n_targets + i] = r;
+  }
+  merge_lists(k, next, [&](int q, float v, int i) {
+    if (lane == 0) {
+      top_ids[row * k + q] = i == STAT_NONE ? -1 : i;
+      top_lp[row * k + q] = i == STAT_NONE ? -INFINITY : ((v - s.m) - lz) + spoilt;
+    }
+  });
+}
+
+// One workgroup of NW waves per part of a row: columns [p chunk, (p + 1) chunk)
+// of row blockIdx.x / parts.  A wave takes tiles of 64 lanes x 16 columns,
+// 16-byte loads, the next tile's in flight while one is worked on; what lies
+// before the first aligned address and past the last whole tile is loaded
+// singly.  Per tile a lane takes its maximum, moves (m, z, t) there and adds its
+// 16 exponentials.
+// The wave's k best so far sit in its lanes 0 .. k - 1.  A tile is looked
+// through only if some lane's maximum is above the k-th of them (a tile's ids are
+// above those before it, so an equal value never displaces); then its best is
+// taken out, at most k times, lowest id first among equals.  For values in no
+// order that happens about k (1 + ln tiles) times a wave.
+template <typename T, int NW>
+__global__ void __launch_bounds__(64 * NW) logprobs_kernel(
+    const T* __restrict__ logits, int V, int mask_id, int n_targets,
+    const int32_t* __restrict__ targets, int k, int parts, int chunk, float* __restrict__ lp,
+    float* __restrict__ entropy, int32_t* __restrict__ top_ids, float* __restrict__ top_lp,
+    Part* __restrict__ out) {
+  constexpr int E = 16, VE = 16 / sizeof(T), NL = E / VE, TILE = 64 * E;
+  __shared__ Part sh[NW];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const size_t row = blockIdx.x / parts;
+  const int p = blockIdx.x % parts;
+  const T* L = logits + row * V;
+  const int lo = p * chunk, hi = min(V, lo + chunk);
+  const int skew = (int)(((uintptr_t)(L + lo) & 15) / sizeof(T));
+  const int body = min(hi, lo + (skew ? VE - skew : 0));       // first aligned column
+  const int tiles = (hi - body) / TILE, tail = body + tiles * TILE;
+
+  Soft s{-INFINITY, 0.f, 0.f};
+  float bv = -INFINITY;                            // lane q < k: the q-th best
+  int bi = STAT_NONE;
+  float bar = k > 0 ? -INFINITY : INFINITY;        // the k-th best's value
+
+  // x: 16 columns of this lane, id(e) the column of x[e], rising with e
+  auto work = [&](float (&x)[E], int base, int end, auto id) {
+    if (mask_id >= base && mask_id < end) {
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (id(e) == mask_id) x[e] = -INFINITY;
+    }
+    float top = x[0];
+#pragma unroll
+    for (int e = 1; e < E; ++e) top = max_nan(top, x[e]);
+    soft_move(s, max_nan(s.m, top));
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const float y = soft_diff(x[e], s.m), ex = exp_neg(y);
+      s.z += ex;
+      s.t += ex * y;
+    }
+    if (__any(!(top <= bar))) {                    // above the bar, or NaN
+      auto best = [&] {                            // NaN logits are not listed
+        float b = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < E; ++e) b = fmaxf(b, x[e]);
+        return b;
+      };
+      top = best();
+      for (int q = 0; q < k; ++q) {
+        const float v = wave_max(top);
+        if (!(v > bar)) break;
+        int at = STAT_NONE;                        // lowest column that holds v
+#pragma unroll
+        for (int e = E - 1; e >= 0; --e)
+          if (x[e] == v) at = id(e);
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) at = min(at, __shfl_xor(at, o, 64));
+        const int place = __popcll(__ballot(lane < k && bv >= v));
+        const float uv = __shfl_up(bv, 1, 64);
+        const int ui = __shfl_up(bi, 1, 64);
+        if (lane == place) { bv = v; bi = at; }
+        else if (lane > place) { bv = uv; bi = ui; }
+        bar = lane_of(bv, k - 1);
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (id(e) == at) x[e] = -INFINITY;
+        top = best();
+      }
+    }
+  };
+  auto single = [&](int from, int to) {            // at most TILE columns, loaded singly
+    float x[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int v = from + 64 * e + lane;
+      x[e] = v < to ? ldf(L + v) : -INFINITY;
+    }
+    work(x, from, to, [&](int e) { return from + 64 * e + lane; });
+  };
+  auto load = [&](int tile, u32x4_t (&r)[NL]) {
+    const T* src = L + body + tile * TILE + lane * VE;
+#pragma unroll
+    for (int j = 0; j < NL; ++j) r[j] = *(const u32x4_t*)(src + j * 64 * VE);
+  };
+
+  if (wave == 0 && body > lo) single(lo, body);
+  if (wave < tiles) {
+    u32x4_t r[NL];
+    load(wave, r);
+    for (int i = wave; i < tiles; i += NW) {
+      float x[E];
+#pragma unroll
+      for (int j = 0; j < NL; ++j)
+#pragma unroll
+        for (int e = 0; e < VE; ++e) x[j * VE + e] = ldf((const T*)&r[j] + e);
+      load(min(i + NW, tiles - 1), r);
+      const int base = body + i * TILE;
+      work(x, base, base + TILE, [&](int e) { return base + (e / VE) * 64 * VE + lane * VE + e % VE; });
+    }
+  }
+  if (wave == tiles % NW && tail < hi) single(tail, hi);
+
+  s = soft_wave(s);
+  if (lane == 0) sh[wave].s = s;
+  if (lane < STAT_K) { sh[wave].v[lane] = bv; sh[wave].id[lane] = bi; }
+  __syncthreads();
+  if (wave != 0) return;
+  s = sh[0].s;
+#pragma unroll
+  for (int w = 1; w < NW; ++w) s = soft_join(s, sh[w].s);
+  auto next = [&](int j, float& v, int& i) {
+    v = lane < NW ? sh[lane].v[j] : -INFINITY;
+    i = lane < NW ? sh[lane].id[j] : STAT_NONE;
+  };
+  if (parts == 1) {
+    row_results(row, s, L, V, mask_id, n_targets, targets, k, lp, entropy, top_ids, top_lp, next);
+  } else {
+    Part* o = out + blockIdx.x;
+    if (lane == 0) o->s = s;
+    merge_lists(k, next, [&](int q, float v, int i) {
+      if (lane == 0) { o->v[q] = v; o->id[q] = i; }
+    });
+  }
+}
+
+// One wave per row: joins the statistics of its parts (at most 64).
+template <typename T>
+__global__ void __launch_bounds__(64) logprobs_join_kernel(
+    const Part* __restrict__ in, int parts, const T* __restrict__ logits, int V, int mask_id,
+    int n_targets, const int32_t* __restrict__ targets, int k, float* __restrict__ lp,
+    float* __restrict__ entropy, int32_t* __restrict__ top_ids, float* __restrict__ top_lp) {
+  const int lane = threadIdx.x;
+  const size_t row = blockIdx.x;
+  const Part* mine = in + row * parts + lane;
+  Soft s{-INFINITY, 0.f, 0.f};
+  if (lane < parts) s = mine->s;
+  s = soft_wave(s);
+  row_results(row, s, logits + row * V, V, mask_id, n_targets, targets, k, lp, entropy, top_ids, top_lp,
+              [&](int j, float& v, int& i) {
+    v = lane < parts ? mine->v[j] : -INFINITY;
+    i = lane < parts ? mine->id[j] : STAT_NONE;
+  });
+}
+
+// Parts of a row: whole rows once they fill the card (4 workgroups to a CU), else
+// parts of at least a tile to each wave.
+struct LogprobsPlan {
+  int parts, chunk;
+};
+static LogprobsPlan logprobs_plan(int rows, int V) {
+  constexpr int LEAST = 4096, WORKGROUPS = 1024;
+  int parts = ceil_div(WORKGROUPS, rows);
+  if (parts > V / LEAST) parts = V / LEAST;
+  if (parts > 64) parts = 64;
+  if (parts <= 1) return {1, V};
+  const int chunk = ceil_div(ceil_div(V, parts), LEAST) * LEAST;
+  return {ceil_div(V, chunk), chunk};
+}
+
 size_t token_logprobs_ws_bytes(int rows, int V, int k) {
-  (void)rows; (void)V; (void)k;
-  return 0;
+  (void)k;
+  if (rows == 0) return 0;
+  const LogprobsPlan p = logprobs_plan(rows, V);
+  return p.parts > 1 ? (size_t)rows * p.parts * sizeof(Part) : 0;
 }
 
 hipError_t launch_token_logprobs(int dtype, int rows, int V, const void* logits, int mask_id,
                                  int n_targets, const int32_t* targets, int k, float* lp,
                                  float* entropy, int32_t* top_ids, float* top_lp, void* ws,
                                  hipStream_t st) {
-  (void)ws;
   if (rows == 0) return hipSuccess;
+  const LogprobsPlan p = logprobs_plan(rows, V);
+  Part* part = (Part*)ws;
   auto go = [&](auto* x) {
     using T = std::remove_cv_t<std::remove_pointer_t<decltype(x)>>;
-    launch(logprobs_kernel<T>, dim3(rows), dim3(256), 0, st, x, V, mask_id, n_targets, targets, k,
-           lp, entropy, top_ids, top_lp);
+    if (V <= 2048)                                  // at most two tiles: a wave to a row
+      launch((logprobs_kernel<T, 1>), dim3(rows), dim3(64), 0, st, x, V, mask_id, n_targets, targets,
+             k, 1, V, lp, entropy, top_ids, top_lp, part);
+    else
+      launch((logprobs_kernel<T, 4>), dim3(rows * p.parts), dim3(256), 0, st, x, V, mask_id, n_targets,
+             targets, k, p.parts, p.chunk, lp, entropy, top_ids, top_lp, part);
+    if (p.parts > 1)
+      launch(logprobs_join_kernel<T>, dim3(rows), dim3(64), 0, st, part, p.parts, x, V, mask_id,
+             n_targets, targets, k, lp, entropy, top_ids, top_lp);
     return hipGetLastError();
   };
   if (dtype == 0) return go((const float*)logits);

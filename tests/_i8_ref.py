@@ -81,14 +81,17 @@ SCORES_REL = 3 * U       # two roundings of the value itself, and one to spare
 
 
 def scores_tol(vocab):
-    """z = sum exp(x - m): a term e^y is off by |y| U (the difference's rounding)
-    and 4 U; weighted by e^y / z, |y| averages to at most ln vocab + 1.  The sum
-    is at most vocab / 256 additions in a chain and 16 joins of 6 U.  t = sum y e^y
-    is at most z (ln vocab + 1) in size and off by the same relative amount and
-    one product.  The logarithm and the quotient round values of up to 40 (4 U
-    each).  To be added for a log probability: x - m and the last difference each
-    round a value of about its own size, which can be thousands: SCORES_REL."""
-    return (math.log(vocab) + 2) * (vocab / 256 + 96 + math.log(vocab) + 1) * U + 40 * 8 * U
+    """z = sum exp(x - m): a term e^y is off by |y| U (the difference's rounding),
+    1.3 |y| U (y log2(e), of a constant that is itself off by a quarter of U) and
+    4 U; weighted by e^y / z, |y| averages to at most ln vocab + 1.  The sum is at
+    most max(32, vocab / 256) additions in a chain, each with a move to another
+    maximum at most every 16th (6 U), and 16 joins of 6 U.  t = sum y e^y is at
+    most z (ln vocab + 1) in size and off by the same relative amount and one
+    product.  The logarithm and the quotient round values of up to 40 (4 U each).
+    To be added for a log probability: x - m and the last difference each round a
+    value of about its own size, which can be thousands: SCORES_REL."""
+    chain = max(32, vocab / 256)
+    return (math.log(vocab) + 2) * (1.4 * chain + 102 + 3 * (math.log(vocab) + 1)) * U + 40 * 8 * U
 
 
 def top(x, k):
