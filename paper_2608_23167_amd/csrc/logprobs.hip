@@ -41,14 +41,41 @@ __device__ __forceinline__ Soft soft_join(Soft a, Soft b) {
   soft_move(b, M);
   return {M, a.z + b.z, a.t + b.t};
 }
-// Over the lanes of a wave, in the same order in every lane.
+// Reductions over a wave by data-parallel moves (about 60 clocks; six shuffles
+// through LDS hardware take six times that): rows of 16 lanes, then across
+// rows, the total in lane 63 and from there, uniform, to all.
+template <class Op>
+__device__ __forceinline__ int wave_reduce(int v, int identity, Op op) {
+#define DPP(ctrl, rows) v = op(v, __builtin_amdgcn_update_dpp(identity, v, ctrl, rows, 0xf, false))
+  DPP(0x111, 0xf);   // row_shr 1, 2, 4, 8
+  DPP(0x112, 0xf);
+  DPP(0x114, 0xf);
+  DPP(0x118, 0xf);
+  DPP(0x142, 0xa);   // lane 15 of rows 0 and 2 to rows 1 and 3
+  DPP(0x143, 0xc);   // lane 31 to rows 2 and 3
+#undef DPP
+  return __builtin_amdgcn_readlane(v, 63);
+}
+template <class Op>
+__device__ __forceinline__ float wave_reduce_f(float v, float identity, Op op) {
+  return __int_as_float(wave_reduce(__float_as_int(v), __float_as_int(identity), [op](int a, int b) {
+    return __float_as_int(op(__int_as_float(a), __int_as_float(b)));
+  }));
+}
+__device__ __forceinline__ float wave_top(float v) {               // not of NaN
+  return wave_reduce_f(v, -INFINITY, [](float a, float b) { return fmaxf(a, b); });
+}
+__device__ __forceinline__ int wave_low(int v) {
+  return wave_reduce(v, STAT_NONE, [](int a, int b) { return min(a, b); });
+}
+// The lane below's value (lane 0 keeps its own).
+__device__ __forceinline__ int from_below(int v) {
+  return __builtin_amdgcn_update_dpp(v, v, 0x138, 0xf, 0xf, false);
+}
 __device__ __forceinline__ Soft soft_wave(Soft a) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    const Soft b{__shfl_xor(a.m, o, 64), __shfl_xor(a.z, o, 64), __shfl_xor(a.t, o, 64)};
-    a = (threadIdx.x & o) ? soft_join(b, a) : soft_join(a, b);
-  }
-  return a;
+  const auto add = [](float x, float y) { return x + y; };
+  soft_move(a, wave_reduce_f(a.m, -INFINITY, [](float x, float y) { return max_nan(x, y); }));
+  return {a.m, wave_reduce_f(a.z, 0.f, add), wave_reduce_f(a.t, 0.f, add)};
 }
 __device__ __forceinline__ float lane_of(float v, int lane) {
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
@@ -63,14 +90,8 @@ __device__ __forceinline__ void merge_lists(int k, Next next, Emit emit) {
   int i, at = 0;
   next(0, v, i);
   for (int q = 0; q < k; ++q) {
-    float bv = v;
-    int bi = i;
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      const float ov = __shfl_xor(bv, o, 64);
-      const int oi = __shfl_xor(bi, o, 64);
-      if (stat_better(ov, oi, bv, bi)) { bv = ov; bi = oi; }
-    }
+    const float bv = wave_top(v);
+    const int bi = wave_low(v == bv ? i : STAT_NONE);
     emit(q, bv, bi);
     if (i == bi && bi != STAT_NONE) {              // ids are different: one lane's
       if (++at < k) next(at, v, i);
@@ -116,11 +137,13 @@ __device__ __forceinline__ void row_results(size_t row, const Soft& s, const T* 
 // before the first aligned address and past the last whole tile is loaded
 // singly.  Per tile a lane takes its maximum, moves (m, z, t) there and adds its
 // 16 exponentials.
-// The wave's k best so far sit in its lanes 0 .. k - 1.  A tile is looked
-// through only if some lane's maximum is above the k-th of them (a tile's ids are
-// above those before it, so an equal value never displaces); then its best is
-// taken out, at most k times, lowest id first among equals.  For values in no
-// order that happens about k (1 + ln tiles) times a wave.
+// The wave's k best so far sit in its lanes 0 .. k - 1; the bar is the k-th.  A
+// tile is looked through only if some lane's maximum is above the bar (its ids are
+// above those before it, so an equal value never displaces), which for values in
+// no order happens k ln(tiles) times a wave.  Where more than k lanes are above
+// it, as in the first tile or in rising rows, the k-th largest of the lanes'
+// maxima is a floor for this tile's candidates.  Each candidate then goes to its
+// place in the list by value and id.
 template <typename T, int NW>
 __global__ void __launch_bounds__(64 * NW) logprobs_kernel(
     const T* __restrict__ logits, int V, int mask_id, int n_targets,
@@ -143,12 +166,14 @@ __global__ void __launch_bounds__(64 * NW) logprobs_kernel(
   int bi = STAT_NONE;
   float bar = k > 0 ? -INFINITY : INFINITY;        // the k-th best's value
 
-  // x: 16 columns of this lane, id(e) the column of x[e], rising with e
-  auto work = [&](float (&x)[E], int base, int end, auto id) {
+  // x[e]: column first + off(e) of this lane, rising with e; lane l's first is
+  // base + l step
+  auto work = [&](float (&x)[E], int base, int end, int step, auto off) {
+    const int first = base + lane * step;
     if (mask_id >= base && mask_id < end) {
 #pragma unroll
       for (int e = 0; e < E; ++e)
-        if (id(e) == mask_id) x[e] = -INFINITY;
+        if (off(e) == mask_id - first) x[e] = -INFINITY;
     }
     float top = x[0];
 #pragma unroll
@@ -160,35 +185,36 @@ __global__ void __launch_bounds__(64 * NW) logprobs_kernel(
       s.z += ex;
       s.t += ex * y;
     }
-    if (__any(!(top <= bar))) {                    // above the bar, or NaN
-      auto best = [&] {                            // NaN logits are not listed
-        float b = -INFINITY;
+    if (__ballot(!(top <= bar)) == 0) return;      // NaN goes on
+    if (__any(top != top)) {                       // NaN logits are not listed
+      top = -INFINITY;
 #pragma unroll
-        for (int e = 0; e < E; ++e) b = fmaxf(b, x[e]);
-        return b;
-      };
-      top = best();
+      for (int e = 0; e < E; ++e) top = fmaxf(top, x[e]);
+    }
+    float floor = bar;
+    if (__popcll(__ballot(top > bar)) > k) {
       for (int q = 0; q < k; ++q) {
-        const float v = wave_max(top);
-        if (!(v > bar)) break;
-        int at = STAT_NONE;                        // lowest column that holds v
-#pragma unroll
-        for (int e = E - 1; e >= 0; --e)
-          if (x[e] == v) at = id(e);
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) at = min(at, __shfl_xor(at, o, 64));
-        const int place = __popcll(__ballot(lane < k && bv >= v));
-        const float uv = __shfl_up(bv, 1, 64);
-        const int ui = __shfl_up(bi, 1, 64);
-        if (lane == place) { bv = v; bi = at; }
-        else if (lane > place) { bv = uv; bi = ui; }
-        bar = lane_of(bv, k - 1);
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (id(e) == at) x[e] = -INFINITY;
-        top = best();
+        floor = wave_top(top);
+        if (lane == __ffsll((unsigned long long)__ballot(top == floor)) - 1) top = -INFINITY;
       }
     }
+    const float over = bar;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      unsigned long long found = __ballot(x[e] > over && x[e] >= floor);
+      while (found) {
+        const int l = __ffsll(found) - 1;
+        found &= found - 1;
+        const float v = lane_of(x[e], l);
+        const int id = base + l * step + off(e);
+        const int place = __popcll(__ballot(lane < k && stat_better(bv, bi, v, id)));
+        const float uv = __int_as_float(from_below(__float_as_int(bv)));
+        const int ui = from_below(bi);
+        if (lane == place) { bv = v; bi = id; }
+        else if (lane > place) { bv = uv; bi = ui; }
+      }
+    }
+    if (k > 0) bar = lane_of(bv, k - 1);
   };
   auto single = [&](int from, int to) {            // at most TILE columns, loaded singly
     float x[E];
@@ -197,7 +223,7 @@ __global__ void __launch_bounds__(64 * NW) logprobs_kernel(
       const int v = from + 64 * e + lane;
       x[e] = v < to ? ldf(L + v) : -INFINITY;
     }
-    work(x, from, to, [&](int e) { return from + 64 * e + lane; });
+    work(x, from, to, 1, [](int e) { return 64 * e; });
   };
   auto load = [&](int tile, u32x4_t (&r)[NL]) {
     const T* src = L + body + tile * TILE + lane * VE;
@@ -217,7 +243,7 @@ __global__ void __launch_bounds__(64 * NW) logprobs_kernel(
         for (int e = 0; e < VE; ++e) x[j * VE + e] = ldf((const T*)&r[j] + e);
       load(min(i + NW, tiles - 1), r);
       const int base = body + i * TILE;
-      work(x, base, base + TILE, [&](int e) { return base + (e / VE) * 64 * VE + lane * VE + e % VE; });
+      work(x, base, base + TILE, VE, [](int e) { return (e / VE) * 64 * VE + e % VE; });
     }
   }
   if (wave == tiles % NW && tail < hi) single(tail, hi);
@@ -271,7 +297,7 @@ struct LogprobsPlan {
 };
 static LogprobsPlan logprobs_plan(int rows, int V) {
   constexpr int LEAST = 4096, WORKGROUPS = 1024;
-  int parts = ceil_div(WORKGROUPS, rows);
+  int parts = WORKGROUPS / rows;
   if (parts > V / LEAST) parts = V / LEAST;
   if (parts > 64) parts = 64;
   if (parts <= 1) return {1, V};
