@@ -17,7 +17,9 @@ from ._lib import check, lib
 
 def _stream(stream) -> C.c_void_p:
     if stream is None:
-        stream = torch.cuda.current_stream()
+        # the handle of torch.cuda.current_stream(), without building the object
+        # (0.1 us instead of 2.7, a quarter of a small call)
+        return C.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
     return C.c_void_p(stream.cuda_stream)
 
 

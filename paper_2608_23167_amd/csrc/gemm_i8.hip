@@ -22,6 +22,16 @@ __device__ __forceinline__ i32x4_t mma_i8(i32x4_t w, i32x4_t a, i32x4_t c) {
   return __builtin_amdgcn_mfma_i32_16x16x64_i8(w, a, c, 0, 0, 0);
 }
 
+__device__ __forceinline__ void put4(float* p, const float (&v)[4]) {
+  *(float4*)p = make_float4(v[0], v[1], v[2], v[3]);
+}
+__device__ __forceinline__ void put4(bf16_t* p, const float (&v)[4]) {
+  *(uint2*)p = uint2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+}
+__device__ __forceinline__ void put4(f16_t* p, const float (&v)[4]) {
+  *(f16x4_t*)p = f16x4_t{(f16_t)v[0], (f16_t)v[1], (f16_t)v[2], (f16_t)v[3]};
+}
+
 // Where a result goes.
 struct I8Out {
   void* p;
@@ -42,22 +52,16 @@ struct I8Out {
 #pragma unroll
     for (int r = 0; r < 4; ++r) s[r] = sw[min(n + r, N - 1)];
   }
-  // columns n .. n + 3 of row m < M, n a multiple of 4
-  __device__ __forceinline__ void store4(int m, int n, const i32x4_t& acc, const float (&s)[4]) const {
-    const float sm = sa[m];
+  // columns n .. n + 3 of row m < M, n a multiple of 4, whose scales are sm and s
+  __device__ __forceinline__ void store4(int m, int n, const i32x4_t& acc, float sm, const float (&s)[4]) const {
+    const size_t i = (size_t)m * N + n;
     float v[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) v[r] = (float)acc[r] * (sm * s[r]);
-    const size_t i = (size_t)m * N + n;
     if (vec && n < N) {
-      if (dtype == 0) {
-        *(float4*)((float*)p + i) = make_float4(v[0], v[1], v[2], v[3]);
-      } else if (dtype == 1) {
-        *(uint2*)((bf16_t*)p + i) = uint2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-      } else {
-        const f16x4_t h = {(f16_t)v[0], (f16_t)v[1], (f16_t)v[2], (f16_t)v[3]};
-        *(f16x4_t*)((f16_t*)p + i) = h;
-      }
+      if (dtype == 0) put4((float*)p + i, v);
+      else if (dtype == 1) put4((bf16_t*)p + i, v);
+      else put4((f16_t*)p + i, v);
     } else {
 #pragma unroll
       for (int r = 0; r < 4; ++r)
@@ -65,6 +69,75 @@ struct I8Out {
     }
   }
 };
+
+// The scales of a wave's tile of FM x FN operands, loaded when the kernel starts:
+// fetched after the products they cost a trip to memory that nothing hides (2 of
+// the 12 us of a launch of one 256 x 256 tile).
+template <int FM, int FN> struct TileScales {
+  float m[FM], n[FN][4];
+  __device__ __forceinline__ void load(const I8Out& out, int row, int col) {
+#pragma unroll
+    for (int i = 0; i < FM; ++i) m[i] = out.sa[min(row + 16 * i, out.M - 1)];
+#pragma unroll
+    for (int j = 0; j < FN; ++j) out.scales4(col + 16 * j, n[j]);
+  }
+  // the loads stay above this point
+  __device__ __forceinline__ void hold() {
+#pragma unroll
+    for (int i = 0; i < FM; ++i) asm volatile("" : "+v"(m[i]));
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) asm volatile("" : "+v"(n[j][r]));
+  }
+};
+
+// A wave's tile: acc[i][j][r] belongs to row m + 16 i, column n + 16 j + r, where n
+// is n0 plus 4 times a quarter of the lane's number.  To the partials of this
+// split, [splits, M, ldp], or out.
+template <int FM, int FN, typename T>
+__device__ __forceinline__ void rows_out(T* p, const i32x4_t (&acc)[FM][FN], int m, int M, int N,
+                                         const TileScales<FM, FN>& sc) {
+#pragma unroll
+  for (int i = 0; i < FM; ++i, p += (size_t)16 * N) {
+    if (m + 16 * i >= M) return;
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+      float v[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) v[r] = (float)acc[i][j][r] * (sc.m[i] * sc.n[j][r]);
+      put4(p + 16 * j, v);
+    }
+  }
+}
+template <int FM, int FN>
+__device__ __forceinline__ void tile_out(const i32x4_t (&acc)[FM][FN], const TileScales<FM, FN>& sc, int m,
+                                         int n0, int n, int split, int* part, int ldp, const I8Out& out) {
+  const int M = out.M;
+  if (part) {
+    int* p = part + ((size_t)split * M + m) * ldp + n;
+#pragma unroll
+    for (int i = 0; i < FM; ++i, p += (size_t)16 * ldp) {
+      if (m + 16 * i >= M) return;
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+        if (n0 + 16 * j < ldp) *(i32x4_t*)(p + 16 * j) = acc[i][j];   // ldp is a multiple of 16
+    }
+    return;
+  }
+  if (out.vec && n0 + 16 * FN <= out.N) {
+    const size_t at = (size_t)m * out.N + n;
+    if (out.dtype == 0) rows_out<FM, FN>((float*)out.p + at, acc, m, M, out.N, sc);
+    else if (out.dtype == 1) rows_out<FM, FN>((bf16_t*)out.p + at, acc, m, M, out.N, sc);
+    else rows_out<FM, FN>((f16_t*)out.p + at, acc, m, M, out.N, sc);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+      if (m + 16 * i < M) out.store4(m + 16 * i, n + 16 * j, acc[i][j], sc.m[i], sc.n[j]);
+}
 
 // ---------------------------------------------------------------------------
 // Any size and alignment
@@ -115,48 +188,36 @@ __global__ void __launch_bounds__(256) gemm_i8_any_kernel(const int8_t* __restri
 // ---------------------------------------------------------------------------
 // Few rows: K split over the waves of a workgroup
 // ---------------------------------------------------------------------------
-// 16 weight rows and up to 16 FM rows to a workgroup of 8 waves.  Wave w takes
-// an eighth of the K-steps of 64 and reads its operands straight from memory
-// (no operand is read by two waves of a workgroup); the eight partial sums
-// join in LDS.  Bound by the weights' bytes: each wave keeps two batches of U
-// K-steps in flight.
-template <int FM, int U>
+// 16 weight rows and up to 16 rows to a workgroup of 8 waves.  Wave w takes an eighth
+// of the K-steps of 64 and reads its operands straight from memory (no operand is
+// read by two waves of a workgroup); the eight partial sums join in LDS.  Bound by
+// the weights' bytes: each wave keeps two batches of U K-steps in flight.
+template <int U>
 __global__ void __launch_bounds__(512) gemm_i8_few_kernel(const int8_t* __restrict__ A,
-                                                          const int8_t* __restrict__ W, int M, int N,
-                                                          int K, I8Out out) {
-  __shared__ i32x4_t red[8][FM][64];
+                                                          const int8_t* __restrict__ W, int K, I8Out out) {
+  __shared__ i32x4_t red[8][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r16 = lane & 15, q = lane >> 4;
-  const int n0 = blockIdx.x * 16, m0 = blockIdx.y * (16 * FM);
+  const int M = out.M, N = out.N, n0 = blockIdx.x * 16;
   const int steps = (K + 63) >> 6, s0 = wave * steps >> 3, s1 = (wave + 1) * steps >> 3;
   const int8_t* wp = W + (size_t)min(n0 + r16, N - 1) * K;
-  const int8_t* ap[FM];
-#pragma unroll
-  for (int i = 0; i < FM; ++i) ap[i] = A + (size_t)min(m0 + 16 * i + r16, M - 1) * K;
-  i32x4_t acc[FM];
-#pragma unroll
-  for (int i = 0; i < FM; ++i) acc[i] = i32x4_t{0, 0, 0, 0};
+  const int8_t* ap = A + (size_t)min(r16, M - 1) * K;
+  i32x4_t acc = {0, 0, 0, 0};
   if (s0 < s1) {
-    i32x4_t w[2][U], a[2][U][FM];
+    i32x4_t w[2][U], a[2][U];
     // K-steps s .. s + U - 1; past s1 or K the activations are 0
-    auto load = [&](int s, i32x4_t (&lw)[U], i32x4_t (&la)[U][FM]) {
+    auto load = [&](int s, i32x4_t (&lw)[U], i32x4_t (&la)[U]) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int k = (s + u) * 64 + q * 16, kc = min(k, K - 16);
-        const bool in = s + u < s1 && k < K;
         lw[u] = *(const i32x4_t*)(wp + kc);
-#pragma unroll
-        for (int i = 0; i < FM; ++i) {
-          const i32x4_t v = *(const i32x4_t*)(ap[i] + kc);
-          la[u][i] = in ? v : i32x4_t{0, 0, 0, 0};
-        }
+        const i32x4_t v = *(const i32x4_t*)(ap + kc);
+        la[u] = s + u < s1 && k < K ? v : i32x4_t{0, 0, 0, 0};
       }
     };
-    auto mma = [&](const i32x4_t (&lw)[U], const i32x4_t (&la)[U][FM]) {
+    auto mma = [&](const i32x4_t (&lw)[U], const i32x4_t (&la)[U]) {
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int i = 0; i < FM; ++i) acc[i] = mma_i8(lw[u], la[u][i], acc[i]);
+      for (int u = 0; u < U; ++u) acc = mma_i8(lw[u], la[u], acc);
     };
     load(s0, w[0], a[0]);
     for (int s = s0; s < s1; s += 2 * U) {
@@ -166,133 +227,15 @@ __global__ void __launch_bounds__(512) gemm_i8_few_kernel(const int8_t* __restri
       mma(w[1], a[1]);
     }
   }
-#pragma unroll
-  for (int i = 0; i < FM; ++i) red[wave][i][lane] = acc[i];
+  red[wave][lane] = acc;
   __syncthreads();
   // output o of the tile: column o % 16 of row o / 16
-  for (int o = threadIdx.x; o < 256 * FM; o += 512) {
-    const int n = o & 15, m = o >> 4;
-    if (m0 + m >= M || n0 + n >= N) continue;
-    int sum = 0;
+  const int o = threadIdx.x, n = o & 15, m = o >> 4;
+  if (o >= 256 || m >= M || n0 + n >= N) return;
+  int sum = 0;
 #pragma unroll
-    for (int v = 0; v < 8; ++v) sum += ((const int*)&red[v][m >> 4][(n >> 2) * 16 + (m & 15)])[n & 3];
-    out.store(m0 + m, n0 + n, sum);
-  }
-}
-
-// ---------------------------------------------------------------------------
-// Cached steps: weights straight into registers, rows through LDS
-// ---------------------------------------------------------------------------
-// 16 FM rows and 16 FN NW weight rows to a workgroup of NW waves; every wave
-// multiplies all the rows with its own 16 FN weight rows.  K-steps of 128.  A
-// weight is read by one wave only, so it goes from memory to the registers of
-// that wave, D K-steps ahead; the rows are read by every wave and go through
-// two LDS buffers, loaded two K-steps ahead and written one ahead, one barrier
-// a K-step.  In LDS a row group's 64 columns are 1 KB in operand order (chunk
-// c of row r at 16 (c % 4) + (r ^ 2 c)): the exclusive or spreads the 8 chunks
-// of a row, written by neighbouring threads, over the banks.
-template <int FM, int FN, int NW, int D>
-__global__ void __launch_bounds__(64 * NW) gemm_i8_stream_kernel(const int8_t* __restrict__ A,
-                                                                 const int8_t* __restrict__ W, int M,
-                                                                 int N, int K, int mt, int n_split,
-                                                                 int* __restrict__ part, int ldp,
-                                                                 I8Out out) {
-  constexpr int T = 64 * NW, BM = 16 * FM, BN = 16 * FN * NW, CH = BM * 8, CA = (CH + T - 1) / T;
-  constexpr int BUF = BM * 128;
-  static_assert(D % 2 == 0, "the two row buffers alternate");
-  __shared__ __attribute__((aligned(1024))) char smem[2 * BUF];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int r16 = lane & 15, q = lane >> 4;
-  int t, mtile, split;
-  tile_of(blockIdx.x, gridDim.x, gridDim.x / n_split, mt, split, t, mtile);
-  const int m0 = mtile * BM, n0 = t * BN + wave * 16 * FN;
-  const int k_steps = (K + 127) >> 7;
-  const int ks0 = (int)((long long)split * k_steps / n_split), ks1 = (int)((long long)(split + 1) * k_steps / n_split);
-  const int nk = ks1 - ks0, kend = min(K, ks1 * 128);
-
-  const int8_t* wp[FN];
-#pragma unroll
-  for (int j = 0; j < FN; ++j) wp[j] = W + (size_t)min(n0 + 16 * j + r16, N - 1) * K;
-  const int8_t* ap[CA];
-  int a_dst[CA], a_col[CA];
-#pragma unroll
-  for (int i = 0; i < CA; ++i) {
-    const int x = min(tid + T * i, CH - 1), r = x >> 3, c = x & 7;   // past the last: the last again
-    ap[i] = A + (size_t)min(m0 + r, M - 1) * K;
-    a_col[i] = c * 16;
-    a_dst[i] = ((r >> 4) * 2 + (c >> 2)) * 1024 + ((c & 3) * 16 + ((r & 15) ^ (2 * c))) * 16;
-  }
-  i32x4_t wr[D][FN][2], ar[2][CA];
-  auto load_w = [&](int x, i32x4_t (&v)[FN][2]) {
-    const int k = (ks0 + min(x, nk - 1)) * 128 + q * 16;
-#pragma unroll
-    for (int j = 0; j < FN; ++j)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) v[j][h] = *(const i32x4_t*)(wp[j] + min(k + 64 * h, K - 16));
-  };
-  // rows of K-step x; 0 past this split's columns, so that steps past the last add nothing
-  auto load_a = [&](int x, i32x4_t (&v)[CA]) {
-#pragma unroll
-    for (int i = 0; i < CA; ++i) {
-      const int k = (ks0 + x) * 128 + a_col[i];
-      const i32x4_t u = *(const i32x4_t*)(ap[i] + min(k, K - 16));
-      v[i] = k < kend ? u : i32x4_t{0, 0, 0, 0};
-    }
-  };
-  auto write_a = [&](const i32x4_t (&v)[CA], int buf) {
-#pragma unroll
-    for (int i = 0; i < CA; ++i)
-      if (CH % T == 0 || tid + T * i < CH) *(i32x4_t*)(smem + buf * BUF + a_dst[i]) = v[i];
-  };
-  i32x4_t acc[FM][FN];
-#pragma unroll
-  for (int i = 0; i < FM; ++i)
-#pragma unroll
-    for (int j = 0; j < FN; ++j) acc[i][j] = i32x4_t{0, 0, 0, 0};
-  auto mma = [&](const i32x4_t (&w)[FN][2], int buf) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const char* src = smem + buf * BUF + h * 1024 + (q * 16 + (r16 ^ (2 * (4 * h + q)))) * 16;
-#pragma unroll
-      for (int i = 0; i < FM; ++i) {
-        const i32x4_t a = *(const i32x4_t*)(src + i * 2048);
-#pragma unroll
-        for (int j = 0; j < FN; ++j) acc[i][j] = mma_i8(w[j][h], a, acc[i][j]);
-      }
-    }
-  };
-
-  load_a(0, ar[0]);
-  load_a(1, ar[1]);
-#pragma unroll
-  for (int u = 0; u < D; ++u) load_w(u, wr[u]);
-  write_a(ar[0], 0);
-  load_a(2, ar[0]);
-  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-  for (int x0 = 0; x0 < nk; x0 += D) {
-#pragma unroll
-    for (int u = 0; u < D; ++u) {
-      const int x = x0 + u;
-      write_a(ar[(u + 1) & 1], (u + 1) & 1);        // K-step x + 1
-      load_a(x + 3, ar[(u + 1) & 1]);
-      mma(wr[u], u & 1);
-      load_w(x + D, wr[u]);
-      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    }
-  }
-#pragma unroll
-  for (int j = 0; j < FN; ++j) {
-    const int n = n0 + 16 * j + 4 * q;
-    float s[4];
-    if (!part) out.scales4(n, s);
-#pragma unroll
-    for (int i = 0; i < FM; ++i) {
-      const int m = m0 + 16 * i + r16;
-      if (m >= M) continue;
-      if (!part) out.store4(m, n, acc[i][j], s);
-      else if (n < ldp) *(i32x4_t*)(part + ((size_t)split * M + m) * ldp + n) = acc[i][j];
-    }
-  }
+  for (int v = 0; v < 8; ++v) sum += ((const int*)&red[v][(n >> 2) * 16 + m])[n & 3];
+  out.store(m, n0 + n, sum);
 }
 
 // ---------------------------------------------------------------------------
@@ -308,61 +251,66 @@ __global__ void __launch_bounds__(64 * NW) gemm_i8_stream_kernel(const int8_t* _
 //   MFMA part:    FM x FN MFMAs on them, barrier.
 // Barriers number the slots: in slot 4t (even) the first group reads half 0
 // of K-step t, in 4t + 1 the second group does while the first multiplies, and
-// so on.  LDS rings: two stages of rows (BM x 128, each half separate), three of
+// so on.  LDS rings: PA stages of rows (BM x 128, each half separate), PA + 1 of
 // weights (BN x 128).  What a copy overwrites and where it is read:
-//   weights t + 2        stage read last in slot 4t - 1, copied in 4t / 4t + 1,
-//                        read from slot 4t + 8 on;
-//   rows t + 1, half 1:  read last in slot 4t - 1, copied in 4t / 4t + 1,
-//                        read from slot 4t + 6 on;
-//   rows t + 2, half 0:  read last in slot 4t + 1, copied in 4t + 2 / 4t + 3,
-//                        read from slot 4t + 8 on.
-// Each wave waits, before the barrier that opens a slot in which the first
-// group reads, until only its copies of the last two phases are in flight.
-// Copies past the last K-step repeat the last one (never read), which keeps
-// the count uniform.
+//   weights t + PA             stage of t - 1, read last in slot 4t - 1, copied in
+//                              4t / 4t + 1, read from slot 4 (t + PA) on;
+//   rows t + PA - 1, half 1:   stage of t - 1, read last in slot 4t - 1, copied in
+//                              4t / 4t + 1, read from slot 4 (t + PA) - 2 on;
+//   rows t + PA, half 0:       stage of t, read last in slot 4t + 1, copied in
+//                              4t + 2 / 4t + 3, read from slot 4 (t + PA) on.
+// A wave waits, before the barrier that opens a slot in which the first group
+// reads, until only its copies of the last 2 (PA - 1) phases are in flight: at
+// the end of (t, half 1) the oldest of those follow rows t + 1, half 0, and at
+// the end of (t, half 0) they follow rows t, half 1.  Copies past the last
+// K-step repeat the last one (never read), which keeps the count uniform.
 //
 // A copy is 1 KB, 16 bytes a lane in order.  One of weights covers 8 rows of
 // 128 bytes, chunk c of row r at place c ^ ((r / 2) % 8); one of rows covers 16
 // rows of 64 bytes, chunk c of row r at place c ^ ((r / 4) % 4): in both the 16
 // rows of a fragment read fall on 16 different 16-byte columns of the banks.
 // What is left of K past the last whole K-step is multiplied from registers.
-template <int BM, int BN, int WM, int WN>
+template <int BM, int BN, int WM, int WN, int PA>
 __global__ void __launch_bounds__(512, 2) gemm_i8_pp_kernel(const int8_t* __restrict__ A,
-                                                            const int8_t* __restrict__ W, int M,
-                                                            int N, int K, int mt, int n_split,
-                                                            int* __restrict__ part, int ldp,
-                                                            I8Out out) {
+                                                            const int8_t* __restrict__ W, int K, int mt,
+                                                            int n_split, int* __restrict__ part,
+                                                            int ldp, I8Out out) {
   static_assert(WM * WN == 8, "8 waves");
   constexpr int RW = BM / WM, CW = BN / WN, FM = RW / 16, FN = CW / 16;
-  constexpr int LA = BM / 128, LW = BN / 64;       // copies per wave: half K-step of rows, K-step of weights
-  static_assert(BM % 128 == 0 && BN % 64 == 0, "whole copies per wave");
+  static_assert(RW % 16 == 0 && CW % 16 == 0, "whole fragments per wave");
+  constexpr int CA = BM / 16, CB = BN / 8;         // copies: half K-step of rows, K-step of weights
+  static_assert(CA % 4 == 0 && CB % 4 == 0, "the waves of a group copy the same number");
+  // of those, per wave of the first and of the second group
+  constexpr int LA0 = (CA + 7) / 8, LA1 = (CA + 3) / 8, LW0 = (CB + 7) / 8, LW1 = (CB + 3) / 8;
   constexpr int A_HALF = BM * 64, A_STAGE = 2 * A_HALF, W_STAGE = BN * 128;   // bytes
-  constexpr int INFLIGHT = LW + 2 * LA;
-  __shared__ __attribute__((aligned(1024))) char smem[2 * A_STAGE + 3 * W_STAGE];
-  char* const Ws = smem + 2 * A_STAGE;
+  constexpr int FLIGHT0 = (PA - 1) * (LW0 + 2 * LA0), FLIGHT1 = (PA - 1) * (LW1 + 2 * LA1);
+  __shared__ __attribute__((aligned(1024))) char smem[PA * A_STAGE + (PA + 1) * W_STAGE];
+  char* const Ws = smem + PA * A_STAGE;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave % WM, wn = wave / WM;
   const bool late = wave >= 4;                     // the second group
   int t, mtile, split;
   tile_of(blockIdx.x, gridDim.x, gridDim.x / n_split, mt, split, t, mtile);
-  const int m0 = mtile * BM, n0 = t * BN;
+  const int M = out.M, N = out.N, m0 = mtile * BM, n0 = t * BN;
   const int k_steps = K >> 7;                      // whole ones
   const int ks0 = (int)((long long)split * k_steps / n_split);
   const int nk = (int)((long long)(split + 1) * k_steps / n_split) - ks0, last = nk - 1;   // nk >= 1 (host-checked)
+  const int rot = t % nk;
+  auto kmap = [rot, nk](int x) { const int y = x + rot; return y >= nk ? y - nk : y; };
 
   // copy sources: a uniform first row, and the lane's row and chunk from there
-  const int8_t *a_src[LA], *w_src[LW];
-  uint32_t a_off[LA], w_off[LW];
+  const int8_t *a_src[LA0], *w_src[LW0];
+  uint32_t a_off[LA0], w_off[LW0];
 #pragma unroll
-  for (int i = 0; i < LA; ++i) {
-    const int b = min(m0 + 16 * (wave * LA + i), M - 1), r = lane >> 2;
+  for (int i = 0; i < LA0; ++i) {
+    const int b = min(m0 + 16 * (wave + 8 * i), M - 1), r = lane >> 2;
     a_src[i] = A + (size_t)b * K + (size_t)ks0 * 128;
     a_off[i] = (uint32_t)min(r, M - 1 - b) * K + (((lane & 3) ^ (r >> 2)) << 4);
   }
 #pragma unroll
-  for (int i = 0; i < LW; ++i) {
-    const int p = wave * LW + i, b = min(n0 + 8 * p, N - 1), r = lane >> 3;
+  for (int i = 0; i < LW0; ++i) {
+    const int p = wave + 8 * i, b = min(n0 + 8 * p, N - 1), r = lane >> 3;
     w_src[i] = W + (size_t)b * K + (size_t)ks0 * 128;
     w_off[i] = (uint32_t)min(r, N - 1 - b) * K + (((lane & 7) ^ (r >> 1) ^ (4 * (p & 1))) << 4);
   }
@@ -370,19 +318,21 @@ __global__ void __launch_bounds__(512, 2) gemm_i8_pp_kernel(const int8_t* __rest
     __builtin_amdgcn_global_load_lds((const void*)(src + off),
                                      (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
   };
-  // half kk of K-step v (rows), into stage v % 2
-  auto issue_a = [&](int v, int kk) {
-    const int vs = min(v, last);
-    char* dst = smem + (v & 1) * A_STAGE + kk * A_HALF + wave * LA * 1024;
+  // half kk of K-step v (rows), into stage `slot`
+  auto issue_a = [&](int v, int kk, int slot) {
+    const int vs = kmap(min(v, last));
+    char* dst = smem + slot * A_STAGE + kk * A_HALF + wave * 1024;
 #pragma unroll
-    for (int i = 0; i < LA; ++i) copy(a_src[i] + (size_t)vs * 128 + kk * 64, a_off[i], dst + i * 1024);
+    for (int i = 0; i < LA0; ++i)
+      if (i < LA1 || !late) copy(a_src[i] + (size_t)vs * 128 + kk * 64, a_off[i], dst + i * 8192);
   };
-  // K-step v (weights), into ring slot `slot`
+  // K-step v (weights), into stage `slot`
   auto issue_w = [&](int v, int slot) {
-    const int vs = min(v, last);
-    char* dst = Ws + slot * W_STAGE + wave * LW * 1024;
+    const int vs = kmap(min(v, last));
+    char* dst = Ws + slot * W_STAGE + wave * 1024;
 #pragma unroll
-    for (int i = 0; i < LW; ++i) copy(w_src[i] + (size_t)vs * 128, w_off[i], dst + i * 1024);
+    for (int i = 0; i < LW0; ++i)
+      if (i < LW1 || !late) copy(w_src[i] + (size_t)vs * 128, w_off[i], dst + i * 8192);
   };
 
   i32x4_t acc[FM][FN];
@@ -396,9 +346,9 @@ __global__ void __launch_bounds__(512, 2) gemm_i8_pp_kernel(const int8_t* __rest
   const int r16 = lane & 15, g4 = lane >> 4;
   const int a_frag = wm * FM * 1024 + r16 * 64 + ((g4 ^ (r16 >> 2)) << 4);
   const int w_lane = r16 * 128 + ((g4 ^ (r16 >> 1)) << 4);        // half 0; half 1: chunk ^ 4
-  auto read = [&](int v, int slot, int kk) {
-    const char* a = smem + (v & 1) * A_STAGE + kk * A_HALF + a_frag;
-    const char* w = Ws + slot * W_STAGE + wn * CW * 128 + (w_lane ^ (kk << 6));
+  auto read = [&](int slot_a, int slot_w, int kk) {
+    const char* a = smem + slot_a * A_STAGE + kk * A_HALF + a_frag;
+    const char* w = Ws + slot_w * W_STAGE + wn * CW * 128 + (w_lane ^ (kk << 6));
 #pragma unroll
     for (int j = 0; j < FN; ++j) wf[j] = *(const i32x4_t*)(w + j * 2048);
 #pragma unroll
@@ -416,38 +366,43 @@ __global__ void __launch_bounds__(512, 2) gemm_i8_pp_kernel(const int8_t* __rest
   auto end_mem = [&]() {
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));   // lgkmcnt(0)
-    if (late) wait_vmcnt<INFLIGHT>();
+    if (late) wait_vmcnt<FLIGHT1>();
     pp_barrier();
   };
   auto end_mma = [&]() {
     __builtin_amdgcn_sched_barrier(0);
-    if (!late) wait_vmcnt<INFLIGHT>();
+    if (!late) wait_vmcnt<FLIGHT0>();
     pp_barrier();
   };
 
-  issue_w(0, 0);
-  issue_a(0, 0);
-  issue_a(0, 1);
-  issue_w(1, 1);
-  issue_a(1, 0);
-  wait_vmcnt<LW + LA>();
+  TileScales<FM, FN> sc;
+  if (!part) sc.load(out, m0 + wm * RW + r16, n0 + wn * CW + 4 * g4);
+#pragma unroll
+  for (int j = 0; j < PA; ++j) {                    // in the order of the loop's copies
+    issue_w(j, j);
+    if (j > 0) issue_a(j - 1, 1, j - 1);
+    issue_a(j, 0, j);
+  }
+  if (late) wait_vmcnt<FLIGHT1>();
+  else wait_vmcnt<FLIGHT0>();
+  if (!part) sc.hold();
   pp_barrier();
   if (late) pp_barrier();
-  int s0 = 0, s2 = 2;                               // ring slots of K-steps v and v + 2
+  int sa = 0, sw = 0;                               // stages of K-step v
   for (int v = 0; v < nk; ++v) {
-    read(v, s0, 0);
-    issue_w(v + 2, s2);
-    issue_a(v + 1, 1);
+    read(sa, sw, 0);
+    issue_w(v + PA, sw == 0 ? PA : sw - 1);
+    issue_a(v + PA - 1, 1, sa == 0 ? PA - 1 : sa - 1);
     end_mem();
     mma();
     end_mma();
-    read(v, s0, 1);
-    issue_a(v + 2, 0);
+    read(sa, sw, 1);
+    issue_a(v + PA, 0, sa);
     end_mem();
     mma();
     end_mma();
-    s2 = s0;
-    s0 = s0 == 2 ? 0 : s0 + 1;
+    sa = sa == PA - 1 ? 0 : sa + 1;
+    sw = sw == PA ? 0 : sw + 1;
   }
   if (!late) pp_barrier();
   wait_vmcnt<0>();                                  // no copy lands after the workgroup ends
@@ -468,27 +423,182 @@ __global__ void __launch_bounds__(512, 2) gemm_i8_pp_kernel(const int8_t* __rest
   }
 
   // acc[i][j][r] = C[m0 + RW wm + 16 i + lane % 16][n0 + CW wn + 16 j + 4 (lane / 16) + r]
+  tile_out(acc, sc, m0 + wm * RW + r16, n0 + wn * CW, n0 + wn * CW + 4 * g4, split, part, ldp, out);
+}
+
+// ---------------------------------------------------------------------------
+// Cached steps: two wave groups that share K
+// ---------------------------------------------------------------------------
+// The alternation above for smaller tiles, where a phase's LDS reads and its
+// barriers would outlast its MFMAs: the waves 0-3 take half 0 of every K-step of
+// 128 and the waves 4-7 half 1, each group the whole BM x BN tile (WM x WN = 4
+// waves), so a wave has a tile twice as large, reads less for each MFMA, and a
+// K-step has 2 slots instead of 4.  The groups' sums join in LDS at the end.
+// Slot 2t: the first group reads half 0 of K-step t while the second multiplies
+// half 1 of t - 1; slot 2t + 1: the other way round.  Rows and weights share a
+// ring of R stages; a wave's copies of K-step t + R - 1, begun in its memory part
+// of t, overwrite the stage of t - 1, read last in slot 2t - 1.  Before the
+// barrier that opens slot 2t + 2 each wave waits until only its copies of the
+// R - 2 latest K-steps are in flight: those of t + 1 have then landed.  All
+// copies are whole lines (8 rows of 128 bytes, chunks placed as above).
+template <int BM, int BN, int WM, int WN, int R>
+__global__ void __launch_bounds__(512, 2) gemm_i8_ks_kernel(const int8_t* __restrict__ A,
+                                                            const int8_t* __restrict__ W, int K, int mt,
+                                                            int n_split, int* __restrict__ part,
+                                                            int ldp, I8Out out) {
+  static_assert(WM * WN == 4 && R >= 3, "4 waves to a group");
+  constexpr int RW = BM / WM, CW = BN / WN, FM = RW / 16, FN = CW / 16;
+  static_assert(RW % 32 == 0 && CW % 16 == 0, "whole fragments per wave, an even number of rows of them");
+  constexpr int CA = BM / 8, CB = BN / 8;          // copies of a K-step
+  static_assert(CA % 4 == 0 && CB % 4 == 0, "the waves of a group copy the same number");
+  // of those, per wave of the first and of the second group
+  constexpr int LA0 = (CA + 7) / 8, LA1 = (CA + 3) / 8, LW0 = (CB + 7) / 8, LW1 = (CB + 3) / 8;
+  constexpr int STAGE = (BM + BN) * 128;           // bytes: rows, then weights
+  constexpr int FLIGHT0 = (R - 2) * (LA0 + LW0), FLIGHT1 = (R - 2) * (LA1 + LW1);
+  static_assert(R * STAGE >= 4 * (FM / 2) * FN * 2 * 1024, "the groups' sums fit the ring");
+  __shared__ __attribute__((aligned(1024))) char smem[R * STAGE];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int w4 = wave & 3, wm = w4 % WM, wn = w4 / WM;
+  const bool late = wave >= 4;                     // the second group
+  int t, mtile, split;
+  tile_of(blockIdx.x, gridDim.x, gridDim.x / n_split, mt, split, t, mtile);
+  const int M = out.M, N = out.N, m0 = mtile * BM, n0 = t * BN;
+  const int k_steps = K >> 7;                      // whole ones
+  const int ks0 = (int)((long long)split * k_steps / n_split);
+  const int nk = (int)((long long)(split + 1) * k_steps / n_split) - ks0, last = nk - 1;   // nk >= 1 (host-checked)
+  const int rot = t % nk;
+  auto kmap = [rot, nk](int x) { const int y = x + rot; return y >= nk ? y - nk : y; };
+
+  // copy sources: a uniform first row, and the lane's row and chunk from there
+  const int8_t *a_src[LA0], *w_src[LW0];
+  uint32_t a_off[LA0], w_off[LW0];
+  const int r8 = lane >> 3;
+  auto chunk = [&](int p) { return (uint32_t)(((lane & 7) ^ (r8 >> 1) ^ (4 * (p & 1))) << 4); };
 #pragma unroll
-  for (int j = 0; j < FN; ++j) {
-    const int n = n0 + wn * CW + 16 * j + 4 * g4;
-    float s[4];
-    if (!part) out.scales4(n, s);
+  for (int i = 0; i < LA0; ++i) {
+    const int p = wave + 8 * i, b = min(m0 + 8 * p, M - 1);
+    a_src[i] = A + (size_t)b * K + (size_t)ks0 * 128;
+    a_off[i] = (uint32_t)min(r8, M - 1 - b) * K + chunk(p);
+  }
 #pragma unroll
-    for (int i = 0; i < FM; ++i) {
-      const int m = m0 + wm * RW + 16 * i + r16;
-      if (m >= M) continue;
-      if (!part) out.store4(m, n, acc[i][j], s);
-      else if (n < ldp) *(i32x4_t*)(part + ((size_t)split * M + m) * ldp + n) = acc[i][j];
+  for (int i = 0; i < LW0; ++i) {
+    const int p = wave + 8 * i, b = min(n0 + 8 * p, N - 1);
+    w_src[i] = W + (size_t)b * K + (size_t)ks0 * 128;
+    w_off[i] = (uint32_t)min(r8, N - 1 - b) * K + chunk(p);
+  }
+  auto copy = [](const int8_t* src, uint32_t off, char* dst) {
+    __builtin_amdgcn_global_load_lds((const void*)(src + off),
+                                     (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
+  };
+  auto issue = [&](int v, int stage) {             // K-step v
+    const size_t k = (size_t)kmap(min(v, last)) * 128;
+    char* dst = smem + stage * STAGE + wave * 1024;
+#pragma unroll
+    for (int i = 0; i < LA0; ++i)
+      if (i < LA1 || !late) copy(a_src[i] + k, a_off[i], dst + i * 8192);
+#pragma unroll
+    for (int i = 0; i < LW0; ++i)
+      if (i < LW1 || !late) copy(w_src[i] + k, w_off[i], dst + BM * 128 + i * 8192);
+  };
+
+  i32x4_t acc[FM][FN];
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j) acc[i][j] = i32x4_t{0, 0, 0, 0};
+  i32x4_t af[FM], wf[FN];
+
+  const int r16 = lane & 15, g4 = lane >> 4;
+  const int frag = r16 * 128 + (((g4 ^ (r16 >> 1)) << 4) ^ (late ? 64 : 0));   // this group's half
+  auto read = [&](int stage) {
+    const char* a = smem + stage * STAGE + wm * RW * 128 + frag;
+    const char* w = smem + stage * STAGE + BM * 128 + wn * CW * 128 + frag;
+#pragma unroll
+    for (int j = 0; j < FN; ++j) wf[j] = *(const i32x4_t*)(w + j * 2048);
+#pragma unroll
+    for (int i = 0; i < FM; ++i) af[i] = *(const i32x4_t*)(a + i * 2048);
+  };
+  auto mma = [&]() {
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j) acc[i][j] = mma_i8(wf[j], af[i], acc[i][j]);
+    __builtin_amdgcn_s_setprio(0);
+  };
+
+  // the groups share the epilogue: the first keeps the fragments i < FM / 2, the
+  // second the rest
+  constexpr int H = FM / 2;
+  TileScales<H, FN> sc;
+  if (!part) sc.load(out, m0 + wm * RW + (late ? 16 * H : 0) + r16, n0 + wn * CW + 4 * g4);
+#pragma unroll
+  for (int j = 0; j < R - 1; ++j) issue(j, j);
+  if (late) wait_vmcnt<FLIGHT1>();
+  else wait_vmcnt<FLIGHT0>();
+  if (!part) sc.hold();
+  pp_barrier();
+  if (late) pp_barrier();
+  int st = 0;                                       // stage of K-step v
+  for (int v = 0; v < nk; ++v) {
+    read(st);
+    issue(v + R - 1, st == 0 ? R - 1 : st - 1);
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));   // lgkmcnt(0)
+    if (late) wait_vmcnt<FLIGHT1>();
+    pp_barrier();
+    mma();
+    __builtin_amdgcn_sched_barrier(0);
+    if (!late) wait_vmcnt<FLIGHT0>();
+    pp_barrier();
+    st = st == R - 1 ? 0 : st + 1;
+  }
+  if (!late) pp_barrier();
+  wait_vmcnt<0>();                                  // no copy lands in the sums below
+
+  if ((K & 127) && split == n_split - 1) {          // the columns past the last whole K-step
+    const int k0 = k_steps * 128 + (late ? 64 : 0);
+    if (k0 < K) {
+      const int k = k0 + 16 * g4, kc = min(k, K - 16);
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+        wf[j] = *(const i32x4_t*)(W + (size_t)min(n0 + wn * CW + 16 * j + r16, N - 1) * K + kc);
+#pragma unroll
+      for (int i = 0; i < FM; ++i) {
+        const i32x4_t u = *(const i32x4_t*)(A + (size_t)min(m0 + wm * RW + 16 * i + r16, M - 1) * K + kc);
+        af[i] = k < K ? u : i32x4_t{0, 0, 0, 0};
+      }
+      mma();
     }
   }
+
+  // each group hands the other's half over
+  __syncthreads();
+  char* mine = smem + (wave * H * FN) * 1024 + lane * 16;
+  const char* theirs = smem + ((wave ^ 4) * H * FN) * 1024 + lane * 16;
+#pragma unroll
+  for (int i = 0; i < H; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j) *(i32x4_t*)(mine + (i * FN + j) * 1024) = late ? acc[i][j] : acc[i + H][j];
+  __syncthreads();
+  i32x4_t sum[H][FN];
+#pragma unroll
+  for (int i = 0; i < H; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+      sum[i][j] = (late ? acc[i + H][j] : acc[i][j]) + *(const i32x4_t*)(theirs + (i * FN + j) * 1024);
+  tile_out(sum, sc, m0 + wm * RW + (late ? 16 * H : 0) + r16, n0 + wn * CW, n0 + wn * CW + 4 * g4, split, part,
+           ldp, out);
 }
 
 // ---------------------------------------------------------------------------
 // Sum of split-K partials
 // ---------------------------------------------------------------------------
 // 4 columns a thread; part is [S, M, ldp] with ldp a multiple of 16.
-__global__ void __launch_bounds__(256) gemm_i8_sum_kernel(const int* __restrict__ part, int S, int M,
-                                                          int ldp, I8Out out) {
+__global__ void __launch_bounds__(256) gemm_i8_sum_kernel(const int* __restrict__ part, int S, int ldp,
+                                                          I8Out out) {
+  const int M = out.M;
   const size_t x = (size_t)blockIdx.x * 256 + threadIdx.x, per = ldp >> 2;
   if (x >= (size_t)M * per) return;
   const int m = (int)(x / per), n = 4 * (int)(x % per);
@@ -497,68 +607,111 @@ __global__ void __launch_bounds__(256) gemm_i8_sum_kernel(const int* __restrict_
   for (int v = 0; v < S; ++v) sum += *(const i32x4_t*)(part + ((size_t)v * M + m) * ldp + n);
   float s[4];
   out.scales4(n, s);
-  out.store4(m, n, sum, s);
+  out.store4(m, n, sum, out.sa[m], s);
 }
 
 // ---------------------------------------------------------------------------
 // Launch choice
 // ---------------------------------------------------------------------------
-enum { I8_FEW = 0, I8_STREAM = 1, I8_PP = 2 };
+// The kernel, tile and number of K splits that should take the least time; for up to
+// I8_FEW_ROWS rows gemm_i8_few_kernel is one of the choices.  A round is a workgroup on
+// each of the 256 CUs (one fits a CU).  In a round of w workgroups a K-step of 128
+// takes step + fill * w / 256 us, the second part for what the CUs share, but the
+// weights come no faster than I8_HBM bytes a us; `fixed` is what a round takes besides.
+// Measured on 160 sizes (40-3840 rows, 700-126464 columns, K 1024-18944) times 12
+// tiles times 6 splits, the weights from memory: the choice takes 0.8% more than
+// the best of them in the mean, 11% at most.  The kernel for few rows took 7.3 us for
+// one row of 4096 x 4096 (64 x 32 tiles 10.3), 12.5 of 4096 x 12288 (15.1), but 27.7 of
+// 24576 x 4096 (64 x 96 tiles 20.4), and for 16 rows 8.6, 17.4 and 38.6 (10.1, 15.5, 20.8).
+static constexpr int I8_FEW_ROWS = 16;
+struct I8Tile {
+  int bm, bn;
+  float step, fill, fixed;
+};
+// number, gemm_i8_pp_kernel (1) or gemm_i8_ks_kernel (0), BM, BN, WM, WN, stages; step, fill, fixed
+#define I8_TILES(X)                              \
+  X(0, 0, 64, 32, 2, 2, 8, 0.18f, 0.02f, 1.9f)   \
+  X(1, 0, 64, 64, 2, 2, 8, 0.24f, 0.03f, 2.4f)   \
+  X(2, 0, 64, 96, 2, 2, 8, 0.24f, 0.07f, 2.9f)   \
+  X(3, 0, 128, 64, 2, 2, 6, 0.29f, 0.10f, 2.4f)  \
+  X(4, 0, 128, 96, 2, 2, 5, 0.30f, 0.17f, 3.0f)  \
+  X(5, 0, 128, 128, 2, 2, 5, 0.34f, 0.20f, 3.3f) \
+  X(6, 0, 128, 160, 2, 2, 4, 0.42f, 0.23f, 3.7f) \
+  X(7, 0, 128, 192, 2, 2, 4, 0.44f, 0.28f, 4.3f) \
+  X(8, 0, 256, 128, 2, 2, 3, 0.54f, 0.32f, 3.4f) \
+  X(9, 1, 128, 256, 2, 4, 2, 0.93f, 0.19f, 2.9f) \
+  X(10, 1, 256, 192, 4, 2, 2, 0.76f, 0.66f, 1.5f) \
+  X(11, 1, 256, 256, 2, 4, 2, 0.88f, 0.55f, 9.4f)
+static constexpr I8Tile I8_TILE[] = {
+#define X(I, PP, BM, BN, WM, WN, R, STEP, FILL, FIXED) {BM, BN, STEP, FILL, FIXED},
+    I8_TILES(X)
+#undef X
+};
+static constexpr int I8_CUS = 256;
+static constexpr float I8_HBM = 6.5e6f;          // bytes a us
+static constexpr float I8_SUM_BYTES = 5.0e6f;    // of partials written and read again, a us
+static constexpr float I8_SUM_US = 1.9f;         // the launch that adds them
+
 struct I8Plan {
-  int kind, tile, split;
+  int tile, split;           // tile -1: gemm_i8_few_kernel
 };
 
 static int i8_ldp(int N) { return (N + 15) & ~15; }
 
-// Tiles of the stream kernel (fm x 16 rows, fn x 16 x nw weight rows) and of
-// the alternating one.
-struct I8Stream { int fm, fn, nw; };
-static constexpr I8Stream I8_STREAMS[] = {{2, 1, 8}, {4, 1, 8}, {8, 1, 8}, {8, 1, 4}, {8, 2, 4}, {16, 2, 4}, {16, 1, 4}, {4, 1, 4}};
-struct I8Pp { int bm, bn; };
-static constexpr I8Pp I8_PPS[] = {{256, 256}, {256, 128}, {128, 256}, {128, 128}};
+// Of gemm_i8_few_kernel: what its workgroups and their weights take, and every row more.
+static float i8_few_cost(int M, int N, int K) {
+  return (2.0e-4f * N + (float)N * K / 5.2e6f) * (1.f + 0.03f * (M - 1));
+}
+
+static float i8_cost(const I8Tile& t, int M, int N, int K, int S) {
+  const long wgs = (long)ceil_div(M, t.bm) * ceil_div(N, t.bn) * S, full = wgs / I8_CUS, rem = wgs % I8_CUS;
+  const float steps = (float)ceil_div(K / 128, S), weights = (float)N * K / I8_HBM / wgs;
+  auto round = [&](long w) {
+    const float mma = steps * (t.step + t.fill * w / I8_CUS), hbm = weights * w;
+    return (mma > hbm ? mma : hbm) + t.fixed;
+  };
+  float us = full * round(I8_CUS);
+  if (rem) us += round(rem);
+  return S > 1 ? us + I8_SUM_US + 8.f * S * M * N / I8_SUM_BYTES : us;
+}
 
 static I8Plan i8_plan(int M, int N, int K) {
 #ifdef SSM_TUNING
-  if (const char* e = getenv("SSM_I8_CFG")) {     // kind:tile:split, for sweeps
+  if (const char* e = getenv("SSM_I8_CFG")) {     // tile:split, for sweeps
     I8Plan p;
-    if (sscanf(e, "%d:%d:%d", &p.kind, &p.tile, &p.split) == 3) return p;
+    if (sscanf(e, "%d:%d", &p.tile, &p.split) == 2) return p;
   }
 #endif
-  if (M <= 32) return {I8_FEW, 0, 1};
-  const int steps = (K + 127) / 128;
-  if (M <= 384 || K < 512) {
-    const int tile = M <= 64 ? 1 : M <= 128 ? 2 : 5;
-    const I8Stream& s = I8_STREAMS[tile];
-    const int tiles = ceil_div(M, 16 * s.fm) * ceil_div(N, 16 * s.fn * s.nw);
-    int S = 1;
-    while (S < 8 && tiles * S * 2 <= 320 && steps / (S * 2) >= 4) S *= 2;
-    return {I8_STREAM, tile, S};
-  }
-  const int tiles = ceil_div(M, 256) * ceil_div(N, 256);
-  int S = 1;
-  while (S < 4 && tiles * (S + 1) <= 256 && (K / 128) / (S + 1) >= 8) ++S;
-  return {I8_PP, 0, S};
+  I8Plan best{-1, 1};
+  float least = M <= I8_FEW_ROWS ? i8_few_cost(M, N, K) : 1e30f;
+  if (K < 128) return best;                        // the tiles need a whole K-step
+  for (int i = 0; i < (int)(sizeof(I8_TILE) / sizeof(I8_TILE[0])); ++i)
+    for (int S : {1, 2, 3, 4, 6, 8}) {
+      if (S > 1 && K / 128 / S < 4) break;
+      const float us = i8_cost(I8_TILE[i], M, N, K, S);
+      if (us < least) {
+        best = {i, S};
+        least = us;
+      }
+    }
+  return best;
 }
 
 size_t gemm_i8_ws_bytes(int M, int N, int K) {
-  if (M == 0 || K % 16) return 0;
+  if (M == 0 || K % 16) return 0;                  // see gemm_i8: no splits without whole chunks
   const I8Plan p = i8_plan(M, N, K);
   return p.split > 1 ? (size_t)p.split * M * i8_ldp(N) * 4 : 0;
 }
 
-template <int FM, int FN, int NW>
-static void launch_stream(const I8Plan& p, int M, int N, int K, const int8_t* a, const int8_t* w,
-                          int* part, const I8Out& out, hipStream_t st) {
-  const int mt = ceil_div(M, 16 * FM);
-  launch((gemm_i8_stream_kernel<FM, FN, NW, 4>), dim3(mt * ceil_div(N, 16 * FN * NW) * p.split),
-         dim3(64 * NW), 0, st, a, w, M, N, K, mt, p.split, part, i8_ldp(N), out);
-}
-template <int BM, int BN, int WM, int WN>
-static void launch_pp(const I8Plan& p, int M, int N, int K, const int8_t* a, const int8_t* w,
-                      int* part, const I8Out& out, hipStream_t st) {
+template <int PP, int BM, int BN, int WM, int WN, int R>
+static void launch_tile(int split, int M, int N, int K, const int8_t* a, const int8_t* w, int* part,
+                        const I8Out& out, hipStream_t st) {
   const int mt = ceil_div(M, BM);
-  launch((gemm_i8_pp_kernel<BM, BN, WM, WN>), dim3(mt * ceil_div(N, BN) * p.split), dim3(512), 0, st,
-         a, w, M, N, K, mt, p.split, part, i8_ldp(N), out);
+  const dim3 grid(mt * ceil_div(N, BN) * split), block(512);
+  if constexpr (PP)
+    launch((gemm_i8_pp_kernel<BM, BN, WM, WN, R>), grid, block, 0, st, a, w, K, mt, split, part, i8_ldp(N), out);
+  else
+    launch((gemm_i8_ks_kernel<BM, BN, WM, WN, R>), grid, block, 0, st, a, w, K, mt, split, part, i8_ldp(N), out);
 }
 
 hipError_t gemm_i8(int M, int N, int K, const int8_t* a, const float* sa, const int8_t* w,
@@ -566,42 +719,23 @@ hipError_t gemm_i8(int M, int N, int K, const int8_t* a, const float* sa, const 
   if (M == 0) return hipSuccess;
   const size_t es = out_dtype == 0 ? 4 : 2;
   const I8Out o{out, out_dtype, N % 4 == 0 && ((uintptr_t)out & (4 * es - 1)) == 0, sa, sw, M, N};
-  if (K % 16 || ((uintptr_t)a & 15) || ((uintptr_t)w & 15)) {
+  if (K % 16 || (K < 128 && M > I8_FEW_ROWS) || ((uintptr_t)a & 15) || ((uintptr_t)w & 15)) {
     launch(gemm_i8_any_kernel, dim3(ceil_div(N, 64), ceil_div(M, 64)), dim3(256), 0, st, a, w, M, N, K, o);
     return hipGetLastError();
   }
   const I8Plan p = i8_plan(M, N, K);
   int* part = p.split > 1 ? (int*)ws : nullptr;
-  if (p.kind == I8_FEW) {
-    if (M <= 16)
-      launch((gemm_i8_few_kernel<1, 4>), dim3(ceil_div(N, 16), 1), dim3(512), 0, st, a, w, M, N, K, o);
-    else
-      launch((gemm_i8_few_kernel<2, 4>), dim3(ceil_div(N, 16), ceil_div(M, 32)), dim3(512), 0, st, a, w, M, N, K, o);
-    return hipGetLastError();
-  }
-  if (p.kind == I8_STREAM) {
-    switch (p.tile) {
-      case 0: launch_stream<2, 1, 8>(p, M, N, K, a, w, part, o, st); break;
-      case 1: launch_stream<4, 1, 8>(p, M, N, K, a, w, part, o, st); break;
-      case 2: launch_stream<8, 1, 8>(p, M, N, K, a, w, part, o, st); break;
-      case 3: launch_stream<8, 1, 4>(p, M, N, K, a, w, part, o, st); break;
-      case 4: launch_stream<8, 2, 4>(p, M, N, K, a, w, part, o, st); break;
-      case 5: launch_stream<16, 2, 4>(p, M, N, K, a, w, part, o, st); break;
-      case 6: launch_stream<16, 1, 4>(p, M, N, K, a, w, part, o, st); break;
-      default: launch_stream<4, 1, 4>(p, M, N, K, a, w, part, o, st); break;
-    }
-  } else {
-    switch (p.tile) {
-      case 0: launch_pp<256, 256, 2, 4>(p, M, N, K, a, w, part, o, st); break;
-      case 1: launch_pp<256, 128, 4, 2>(p, M, N, K, a, w, part, o, st); break;
-      case 2: launch_pp<128, 256, 2, 4>(p, M, N, K, a, w, part, o, st); break;
-      default: launch_pp<128, 128, 4, 2>(p, M, N, K, a, w, part, o, st); break;
-    }
+  switch (p.tile) {
+#define X(I, PP, BM, BN, WM, WN, R, STEP, FILL, FIXED) \
+  case I: launch_tile<PP, BM, BN, WM, WN, R>(p.split, M, N, K, a, w, part, o, st); break;
+    I8_TILES(X)
+#undef X
+    default:
+      launch(gemm_i8_few_kernel<4>, dim3(ceil_div(N, 16)), dim3(512), 0, st, a, w, K, o);
   }
   if (part) {
     const size_t n = (size_t)M * (i8_ldp(N) / 4);
-    launch(gemm_i8_sum_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, part, p.split, M,
-           i8_ldp(N), o);
+    launch(gemm_i8_sum_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, part, p.split, i8_ldp(N), o);
   }
   return hipGetLastError();
 }
