@@ -419,9 +419,6 @@ __device__ __forceinline__ void tile_epilogue(const Pol& pol, const float* Cs, i
 __device__ __forceinline__ void lds_handover_barrier() {
   asm volatile("s_barrier" ::: "memory");
 }
-__device__ __forceinline__ void lds_written_barrier() {
-  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-}
 
 // Warp-specialised workgroup of 8 waves, BM rows (128 or 256; 64 and 192 in a
 // tuning build) x BN columns.

@@ -142,44 +142,86 @@ __device__ __forceinline__ void tile_out(const i32x4_t (&acc)[FM][FN], const Til
 // ---------------------------------------------------------------------------
 // Any size and alignment
 // ---------------------------------------------------------------------------
-// 64 x 64 tiles, 64 columns of K at a time through LDS byte by byte, four
-// products an instruction.
+// 64 x 64 tiles, 4 waves of 32 x 32 each, K-steps of 128 through two LDS buffers, the
+// loads two K-steps ahead.  16-byte loads at any address; the bytes of a chunk that
+// K ends in are loaded singly, so that nothing past a row is read.  In LDS a group of
+// 16 rows' 64 columns are 1 KB in operand order, chunk c of row r at 16 (c % 4) +
+// (r ^ 2 c): the exclusive or spreads the 8 chunks of a row, written by neighbouring
+// threads, over the banks.
+typedef i32x4_t i32x4_any_t __attribute__((aligned(1)));
+
+__device__ __forceinline__ i32x4_t chunk_any(const int8_t* row, int k, int K) {
+  if (k + 16 <= K) return *(const i32x4_any_t*)(row + k);
+  uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    if (k + i < K) w[i >> 2] |= (uint32_t)(uint8_t)row[k + i] << (8 * (i & 3));
+  return i32x4_t{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
+}
+
 __global__ void __launch_bounds__(256) gemm_i8_any_kernel(const int8_t* __restrict__ A,
-                                                          const int8_t* __restrict__ W, int M, int N,
-                                                          int K, I8Out out) {
-  __shared__ int As[64][17], Ws[64][17];
-  const int tid = threadIdx.x, tm = tid >> 4, tn = tid & 15;
-  const int m0 = blockIdx.y * 64, n0 = blockIdx.x * 64;
-  int acc[4][4] = {};
-  for (int k0 = 0; k0 < K; k0 += 64) {
+                                                          const int8_t* __restrict__ W, int K, I8Out out) {
+  constexpr int BUF = 64 * 128;
+  __shared__ __attribute__((aligned(1024))) char smem[2][2][BUF];   // buffer, operand
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int r16 = lane & 15, q = lane >> 4;
+  const int M = out.M, N = out.N, m0 = blockIdx.y * 64, n0 = blockIdx.x * 64;
+  const int nk = (K + 127) >> 7;
+  const int8_t* src[2][2];
+  int dst[2], col[2];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int r = (tid >> 6) + 4 * i, c = tid & 63, k = k0 + c;
-      const int8_t a = (m0 + r < M && k < K) ? A[(size_t)(m0 + r) * K + k] : (int8_t)0;
-      const int8_t w = (n0 + r < N && k < K) ? W[(size_t)(n0 + r) * K + k] : (int8_t)0;
-      ((int8_t*)As[r])[c] = a;
-      ((int8_t*)Ws[r])[c] = w;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int c = 0; c < 16; ++c) {
-      int a[4], w[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) { a[i] = As[tm + 16 * i][c]; w[i] = Ws[tn + 16 * i][c]; }
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_sdot4(a[i], w[j], acc[i][j], false);
-    }
-    __syncthreads();
+  for (int i = 0; i < 2; ++i) {
+    const int x = tid + 256 * i, r = x >> 3, c = x & 7;
+    src[0][i] = A + (size_t)min(m0 + r, M - 1) * K;
+    src[1][i] = W + (size_t)min(n0 + r, N - 1) * K;
+    col[i] = c * 16;
+    dst[i] = ((r >> 4) * 2 + (c >> 2)) * 1024 + ((c & 3) * 16 + ((r & 15) ^ (2 * c))) * 16;
   }
+  i32x4_t v[2][2];
+  auto load = [&](int x) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+    for (int o = 0; o < 2; ++o)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int m = m0 + tm + 16 * i, n = n0 + tn + 16 * j;
-      if (m < M && n < N) out.store(m, n, acc[i][j]);
+      for (int i = 0; i < 2; ++i) v[o][i] = chunk_any(src[o][i], x * 128 + col[i], K);
+  };
+  auto write = [&](int buf) {
+#pragma unroll
+    for (int o = 0; o < 2; ++o)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) *(i32x4_t*)(smem[buf][o] + dst[i]) = v[o][i];
+  };
+  const int wm = (wave & 1) * 2, wn = (wave >> 1) * 2;             // first 16-row group of the wave
+  i32x4_t acc[2][2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) acc[i][j] = i32x4_t{0, 0, 0, 0};
+  load(0);
+  write(0);
+  load(1);                                          // past K: zeros
+  __syncthreads();
+  for (int x = 0; x < nk; ++x) {
+    write((x + 1) & 1);                             // read last in x - 1
+    load(x + 2);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int at = h * 1024 + (q * 16 + (r16 ^ (2 * (4 * h + q)))) * 16;
+      i32x4_t a[2], w[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) a[i] = *(const i32x4_t*)(smem[x & 1][0] + (wm + i) * 2048 + at);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) w[j] = *(const i32x4_t*)(smem[x & 1][1] + (wn + j) * 2048 + at);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[i][j] = mma_i8(w[j], a[i], acc[i][j]);
     }
+    lds_written_barrier();
+  }
+  TileScales<2, 2> sc;
+  const int m = m0 + 16 * wm + r16, n = n0 + 16 * wn;
+  sc.load(out, m, n + 4 * q);
+  tile_out(acc, sc, m, n, n + 4 * q, 0, nullptr, 0, out);
 }
 
 // The kernels below need K a multiple of 16 and 16-byte aligned operands: every
@@ -720,7 +762,7 @@ hipError_t gemm_i8(int M, int N, int K, const int8_t* a, const float* sa, const 
   const size_t es = out_dtype == 0 ? 4 : 2;
   const I8Out o{out, out_dtype, N % 4 == 0 && ((uintptr_t)out & (4 * es - 1)) == 0, sa, sw, M, N};
   if (K % 16 || (K < 128 && M > I8_FEW_ROWS) || ((uintptr_t)a & 15) || ((uintptr_t)w & 15)) {
-    launch(gemm_i8_any_kernel, dim3(ceil_div(N, 64), ceil_div(M, 64)), dim3(256), 0, st, a, w, M, N, K, o);
+    launch(gemm_i8_any_kernel, dim3(ceil_div(N, 64), ceil_div(M, 64)), dim3(256), 0, st, a, w, K, o);
     return hipGetLastError();
   }
   const I8Plan p = i8_plan(M, N, K);

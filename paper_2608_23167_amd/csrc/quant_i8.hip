@@ -60,20 +60,22 @@ template <int V, typename T> __device__ __forceinline__ void load_v(const T* p, 
     const float4 f = *(const float4*)p;
     v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
   } else {
-    const uint2 u = *(const uint2*)p;
+    using U = std::conditional_t<V == 8, u32x4_t, uint2>;
+    const U u = *(const U*)p;
     const T* e = (const T*)&u;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = ldf(e + i);
+    for (int i = 0; i < V; ++i) v[i] = ldf(e + i);
   }
 }
 template <int V> __device__ __forceinline__ void store_codes(int8_t* q, const float (&y)[V], float inv) {
   if constexpr (V == 1) {
     *q = code(y[0], inv);
   } else {
-    uint32_t w = 0;
+    uint32_t w[V / 4] = {};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w |= (uint32_t)(uint8_t)code(y[i], inv) << (8 * i);
-    *(uint32_t*)q = w;
+    for (int i = 0; i < V; ++i) w[i >> 2] |= (uint32_t)(uint8_t)code(y[i], inv) << (8 * (i & 3));
+    if constexpr (V == 8) *(uint2*)q = uint2{w[0], w[1]};
+    else *(uint32_t*)q = w[0];
   }
 }
 
@@ -276,6 +278,15 @@ static hipError_t quant_t(int rows, int d, bool sw, const T* x, int8_t* q, float
     else launch((quant_rows_kernel<T, false, V, NV, TPR>), grid, block, 0, st, x, rows, d, q, scale);   \
     return hipGetLastError();                                                                        \
   } while (0)
+  if constexpr (sizeof(T) == 2) {                  // 16-byte loads of 16-bit rows
+    if (d % 8 == 0 && aligned(x, 16) && aligned(q, 8)) {
+      if (d <= 1024) QUANT(8, 2, 64);
+      if (d <= 4096) QUANT(8, 2, 256);
+      if (d <= 8192) QUANT(8, 1, 1024);
+      if (d <= 16384) QUANT(8, 2, 1024);
+      if (d <= 32768) QUANT(8, 4, 1024);
+    }
+  }
   ROWS_DISPATCH(QUANT);
 #undef QUANT
   if (sw) launch(quant_i8_kernel<T, true>, dim3(rows), dim3(256), 0, st, x, d, q, scale);

@@ -36,4 +36,10 @@ __device__ __forceinline__ void pp_barrier() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
+// A workgroup barrier once this wave's LDS accesses are done; its loads from memory
+// stay in flight.
+__device__ __forceinline__ void lds_written_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
 }  // namespace ssm
