@@ -592,7 +592,8 @@ static constexpr int32_t I8_MAX_K = (1 << 17) - 1;
 int32_t ssm_norm_i8(int32_t rows, int32_t d, const float* d_x, const void* d_delta,
                     int32_t delta_dtype, const void* d_gain, int32_t gain_dtype, float eps,
                     float* d_resid, int8_t* d_q, float* d_scale, void* stream) {
-  if (rows < 0 || rows > I8_MAX_ROWS || d < 1) return fail(SSM_E_INVAL, "bad sizes (rows %d, d %d)", rows, d);
+  if (rows < 0 || rows > I8_MAX_ROWS || d < 1 || d > (1 << 30))
+    return fail(SSM_E_INVAL, "bad sizes (rows %d, d %d)", rows, d);
   if (d_delta && !float_dtype(delta_dtype)) return fail(SSM_E_INVAL, "unknown delta_dtype %d", delta_dtype);
   if (gain_dtype != SSM_DT_F32 && gain_dtype != SSM_DT_BF16)
     return fail(SSM_E_INVAL, "gain_dtype must be SSM_DT_F32 or SSM_DT_BF16 (got %d)", gain_dtype);

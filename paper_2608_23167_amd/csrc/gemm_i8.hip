@@ -783,3 +783,21 @@ hipError_t gemm_i8(int M, int N, int K, const int8_t* a, const float* sa, const 
 }
 
 }  // namespace ssm
+
+// The launch that sizes with aligned operands get, for tests of the choice: rows and
+// columns of the tile (16 x 16: gemm_i8_few_kernel, 0 x 0: gemm_i8_any_kernel), K splits.
+#ifdef SSM_DEBUG
+extern "C" int32_t ssm_debug_gemm_i8_plan(int32_t M, int32_t N, int32_t K, int32_t* out) {
+  using namespace ssm;
+  if (K % 16 || (K < 128 && M > I8_FEW_ROWS)) {
+    out[0] = out[1] = 0;
+    out[2] = 1;
+    return 0;
+  }
+  const I8Plan p = i8_plan(M, N, K);
+  out[0] = p.tile < 0 ? 16 : I8_TILE[p.tile].bm;
+  out[1] = p.tile < 0 ? 16 : I8_TILE[p.tile].bn;
+  out[2] = p.split;
+  return 0;
+}
+#endif

@@ -30,21 +30,29 @@ def _offset(t, elements):
     return v
 
 
+def _guarded(rows, d):
+    """q [rows, d] and scale [rows], with a row behind the last that must be left as it was."""
+    return torch.full((rows + 1, d), 99, dtype=I8, device=DEV), torch.full((rows + 1,), -1.0, device=DEV)
+
+
+def _unguarded(q, s):
+    assert bool((q[-1] == 99).all()) and float(s[-1]) == -1
+    return q[:-1], s[:-1]
+
+
 def _norm(x, gain, eps, delta=None, resid=None):
     from paper_2608_23167_amd import api
-    q = torch.full(x.shape, 99, dtype=I8, device=DEV)
-    s = torch.full((x.shape[0],), -1.0, device=DEV)
-    api.ssm_norm_i8(x, gain, eps, q, s, delta=delta, resid=resid)
-    return q, s
+    q, s = _guarded(*x.shape)
+    api.ssm_norm_i8(x, gain, eps, q[:-1], s[:-1], delta=delta, resid=resid)
+    return _unguarded(q, s)
 
 
 def _quant(x, swiglu=False):
     from paper_2608_23167_amd import api
     d = x.shape[1] // 2 if swiglu else x.shape[1]
-    q = torch.full((x.shape[0], d), 99, dtype=I8, device=DEV)
-    s = torch.full((x.shape[0],), -1.0, device=DEV)
-    api.ssm_quant_i8(x, q, s, swiglu=swiglu)
-    return q, s
+    q, s = _guarded(x.shape[0], d)
+    api.ssm_quant_i8(x, q[:-1], s[:-1], swiglu=swiglu)
+    return _unguarded(q, s)
 
 
 def _gemm(a, sa, w, sw, dtype, ws_extra=0):
@@ -118,6 +126,16 @@ def test_norm_special_rows(gpu, d):
     R.check_codes(q[ok], s[ok], R.norm(x[ok], torch.ones(d, device=DEV), 1e-5), R.norm_rel(d))
 
 
+def test_norm_without_eps(gpu):
+    """Without eps a row of zeros has no norm: NaN scale, codes 0; other rows are not touched by it."""
+    x = _rand(1, 3, 200)
+    x[1] = 0
+    q, s = _norm(x, torch.ones(200, device=DEV), 0.0)
+    assert bool(torch.isnan(s[1])) and not bool(q[1].any())
+    ok = torch.tensor([0, 2], device=DEV)
+    R.check_codes(q[ok], s[ok], R.norm(x[ok], torch.ones(200, device=DEV), 0.0), R.norm_rel(200))
+
+
 # ---- rows to codes --------------------------------------------------------------
 @pytest.mark.parametrize("rows,d", [(1, 1), (1, 12288), (3, 127), (5, 128), (17, 1000), (240, 512),
                                     (7, 3584), (2, 18944), (3, 20001), (2, 40000)])
@@ -173,8 +191,15 @@ SIZES = [(1, 1, 1), (1, 16, 16), (1, 4096, 4096), (2, 33, 48), (5, 100, 100), (1
          (250, 255, 1024), (256, 256, 256), (257, 513, 640), (376, 1536, 512), (513, 3584, 1152),
          (700, 300, 1001), (1127, 896, 2368), (2049, 1030, 400)]
 
+# every tile, and every number of K splits, with rows, columns and K that end inside a tile
+TILE_SIZES = [(30, 1008, 352), (1101, 157, 3904), (1084, 129, 3088), (68, 186, 2608), (191, 198, 3248),
+              (25, 126, 5696), (1382, 603, 320), (950, 2114, 320), (1033, 9943, 1360), (27, 18307, 416),
+              (949, 1156, 336), (517, 3333, 576), (1064, 2780, 528), (2498, 1597, 784), (262, 14266, 1168),
+              (2105, 2519, 816), (301, 21310, 944), (2379, 277, 5648), (641, 663, 6624), (885, 587, 4768),
+              (82, 1514, 4784), (79, 5656, 6160), (68, 8503, 6288)]
 
-@pytest.mark.parametrize("m,n,k", SIZES)
+
+@pytest.mark.parametrize("m,n,k", SIZES + TILE_SIZES)
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
 def test_gemm(gpu, m, n, k, dtype):
     a, w = _codes(m + k, m, k), _codes(n + 7, n, k)

@@ -21,6 +21,7 @@ def _norm(rows=2, d=8, x=P1, delta=P1, ddt=0, gain=P1, gdt=1, eps=1e-5, resid=P1
 
 @pytest.mark.parametrize("kw,word", [
     (dict(rows=-1), "sizes"), (dict(d=0), "sizes"), (dict(d=-4), "sizes"), (dict(rows=(1 << 24) + 1), "sizes"),
+    (dict(d=(1 << 30) + 1), "sizes"),
     (dict(ddt=3), "delta_dtype"), (dict(gdt=2), "gain_dtype"), (dict(gdt=-1), "gain_dtype"),
     (dict(eps=-1.0), "eps"), (dict(eps=float("nan")), "eps"), (dict(eps=float("inf")), "eps"),
     (dict(x=NULL), "null"), (dict(gain=NULL), "null"), (dict(q=NULL), "null"), (dict(s=NULL), "null")])
