@@ -30,8 +30,12 @@ def _run(x, ids, mask_id, k, stream=None):
     tlp = torch.full((rows + 1, max(k, 1)), 7.0, device=DEV)
     need = api.ssm_token_logprobs_workspace_size(rows, vocab, k)
     ws = torch.full((need,), 0xff, dtype=torch.uint8, device=DEV) if need else None
+    if stream is not None:                         # after the fills above, before the checks below
+        stream.wait_stream(torch.cuda.current_stream())
     api.ssm_token_logprobs(x, ids, mask_id, k, lp[:rows] if t else None, ent[:rows],
                            top[:rows] if k else None, tlp[:rows] if k else None, ws, stream=stream)
+    if stream is not None:
+        torch.cuda.current_stream().wait_stream(stream)
     assert bool((lp[rows:] == 7).all()) and bool((ent[rows:] == 7).all())
     assert bool((top[rows:] == -7).all()) and bool((tlp[rows:] == 7).all())
     return lp[:rows], ent[:rows], top[:rows], tlp[:rows]
@@ -235,8 +239,6 @@ def test_captured_and_on_another_stream(gpu, rows, vocab):
         torch.cuda.synchronize()
         for t, w in zip((lp, ent, top, tlp), want):
             assert torch.equal(t, w)
-    st = torch.cuda.Stream()
-    st.wait_stream(torch.cuda.current_stream())
-    other = _run(x, ids, 0, 4, stream=st)
-    torch.cuda.synchronize()
-    assert torch.equal(other[2], top)
+    other = _run(x, ids, 0, 4, stream=torch.cuda.Stream())
+    for t, w in zip(other, (lp, ent, top, tlp)):
+        assert torch.equal(t, w)
