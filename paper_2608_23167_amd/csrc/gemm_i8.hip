@@ -110,6 +110,24 @@ __device__ __forceinline__ void rows_out(T* p, const i32x4_t (&acc)[FM][FN], int
     }
   }
 }
+// The same element by element: a tile of the last columns, or rows that are not aligned.
+template <int FM, int FN, typename T>
+__device__ __forceinline__ void rows_edge(T* p, bool bf, const i32x4_t (&acc)[FM][FN], int m, int M, int n, int N,
+                                          const TileScales<FM, FN>& sc) {
+#pragma unroll
+  for (int i = 0; i < FM; ++i, p += (size_t)16 * N) {
+    if (m + 16 * i >= M) return;
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        if (n + 16 * j + r >= N) continue;
+        const float v = (float)acc[i][j][r] * (sc.m[i] * sc.n[j][r]);
+        if constexpr (std::is_same<T, float>::value) p[16 * j + r] = v;
+        else p[16 * j + r] = bf ? f2bf(v) : __builtin_bit_cast(uint16_t, (f16_t)v);
+      }
+  }
+}
 template <int FM, int FN>
 __device__ __forceinline__ void tile_out(const i32x4_t (&acc)[FM][FN], const TileScales<FM, FN>& sc, int m,
                                          int n0, int n, int split, int* part, int ldp, const I8Out& out) {
@@ -125,18 +143,15 @@ __device__ __forceinline__ void tile_out(const i32x4_t (&acc)[FM][FN], const Til
     }
     return;
   }
+  const size_t at = (size_t)m * out.N + n;
   if (out.vec && n0 + 16 * FN <= out.N) {
-    const size_t at = (size_t)m * out.N + n;
     if (out.dtype == 0) rows_out<FM, FN>((float*)out.p + at, acc, m, M, out.N, sc);
     else if (out.dtype == 1) rows_out<FM, FN>((bf16_t*)out.p + at, acc, m, M, out.N, sc);
     else rows_out<FM, FN>((f16_t*)out.p + at, acc, m, M, out.N, sc);
     return;
   }
-#pragma unroll
-  for (int i = 0; i < FM; ++i)
-#pragma unroll
-    for (int j = 0; j < FN; ++j)
-      if (m + 16 * i < M) out.store4(m + 16 * i, n + 16 * j, acc[i][j], sc.m[i], sc.n[j]);
+  if (out.dtype == 0) rows_edge<FM, FN>((float*)out.p + at, 0, acc, m, M, n, out.N, sc);
+  else rows_edge<FM, FN>((uint16_t*)out.p + at, out.dtype == 1, acc, m, M, n, out.N, sc);
 }
 
 // ---------------------------------------------------------------------------
