@@ -504,7 +504,11 @@ __global__ void __launch_bounds__(512, 2) gemm_i8_pp_kernel(const int8_t* __rest
 // of t, overwrite the stage of t - 1, read last in slot 2t - 1.  Before the
 // barrier that opens slot 2t + 2 each wave waits until only its copies of the
 // R - 2 latest K-steps are in flight: those of t + 1 have then landed.  All
-// copies are whole lines (8 rows of 128 bytes, chunks placed as above).
+// copies are whole lines (8 rows of 128 bytes, chunks placed as above).  Weights that
+// one workgroup reads (a single row tile, K not split) are loaded nontemporal, which
+// leaves the caches to the rows: 120 x 24576 x 4096 29.5 -> 27.7 us, 40 rows 21.6 ->
+// 20.1, 120 x 126464 x 4096 124.6 -> 120.4; with two row tiles or splits it costs
+// (376 x 12288 x 4096 28.9 -> 31.9, 120 x 4096 x 12288 20.9 -> 23.5).
 template <int BM, int BN, int WM, int WN, int R>
 __global__ void __launch_bounds__(512, 2) gemm_i8_ks_kernel(const int8_t* __restrict__ A,
                                                             const int8_t* __restrict__ W, int K, int mt,
@@ -555,6 +559,11 @@ __global__ void __launch_bounds__(512, 2) gemm_i8_ks_kernel(const int8_t* __rest
     __builtin_amdgcn_global_load_lds((const void*)(src + off),
                                      (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
   };
+  auto copy_once = [](const int8_t* src, uint32_t off, char* dst) {        // 2: nontemporal
+    __builtin_amdgcn_global_load_lds((const void*)(src + off),
+                                     (__attribute__((address_space(3))) void*)dst, 16, 0, 2);
+  };
+  const bool once = mt == 1 && n_split == 1;
   auto issue = [&](int v, int stage) {             // K-step v
     const size_t k = (size_t)kmap(min(v, last)) * 128;
     char* dst = smem + stage * STAGE + wave * 1024;
@@ -563,7 +572,10 @@ __global__ void __launch_bounds__(512, 2) gemm_i8_ks_kernel(const int8_t* __rest
       if (i < LA1 || !late) copy(a_src[i] + k, a_off[i], dst + i * 8192);
 #pragma unroll
     for (int i = 0; i < LW0; ++i)
-      if (i < LW1 || !late) copy(w_src[i] + k, w_off[i], dst + BM * 128 + i * 8192);
+      if (i < LW1 || !late) {
+        if (once) copy_once(w_src[i] + k, w_off[i], dst + BM * 128 + i * 8192);
+        else copy(w_src[i] + k, w_off[i], dst + BM * 128 + i * 8192);
+      }
   };
 
   i32x4_t acc[FM][FN];
