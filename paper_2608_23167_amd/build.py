@@ -16,8 +16,8 @@ and closed-form host paths.
 
 `--tuning` builds a separate library (libssm_tuning.so, objects in
 _build_tuning/) with SSM_TUNING defined: its GEMM launch choices can be
-overridden through the SSM_GEMM_CFG / SSM_GEMM_KROT environment variables
-for tile sweeps.  The product library never reads them.
+overridden through the SSM_GEMM_CFG / SSM_GEMM_KROT and SSM_I8_CFG
+environment variables for tile sweeps.  The product library never reads them.
 """
 from __future__ import annotations
 

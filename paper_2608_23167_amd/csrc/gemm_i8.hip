@@ -248,7 +248,8 @@ __global__ void __launch_bounds__(256) gemm_i8_any_kernel(const int8_t* __restri
 // 16 weight rows and up to 16 rows to a workgroup of 8 waves.  Wave w takes an eighth
 // of the K-steps of 64 and reads its operands straight from memory (no operand is
 // read by two waves of a workgroup); the eight partial sums join in LDS.  Bound by
-// the weights' bytes: each wave keeps two batches of U K-steps in flight.
+// the weights' bytes: each wave keeps two batches of U K-steps in flight.  One row of
+// 4096 x 4096: 6.0 us (2.8 TB/s; launch and one trip to memory are 4 of them).
 template <int U>
 __global__ void __launch_bounds__(512) gemm_i8_few_kernel(const int8_t* __restrict__ A,
                                                           const int8_t* __restrict__ W, int K, I8Out out) {
@@ -330,6 +331,10 @@ __global__ void __launch_bounds__(512) gemm_i8_few_kernel(const int8_t* __restri
 // 16-19 and 28-31) together, which counters say is how they go: with r / 4 for
 // half_place(r), even for the first grouping only, 13% of the clocks were conflicts.
 // What is left of K past the last whole K-step is multiplied from registers.
+// 3840 x 24576 x 4096: 361 us, 2140 TOP/s; the MFMAs are busy 53% of the clocks, and the
+// clock gives way to the power of that (1.9 GHz).  Of a round of 61 us 10 pass before the
+// first product and after the last; workgroups that stay for several tiles and start
+// the next one's copies before they store were tried: the loop around it all spilled.
 __device__ __forceinline__ int half_place(int r) {      // 0, 2, 3, 1 for r / 4 = 0 .. 3
   return ((r >> 2) & 1) * 2 ^ ((r >> 3) & 1) * 3;
 }
@@ -509,6 +514,10 @@ __global__ void __launch_bounds__(512, 2) gemm_i8_pp_kernel(const int8_t* __rest
 // leaves the caches to the rows: 120 x 24576 x 4096 29.5 -> 27.7 us, 40 rows 21.6 ->
 // 20.1, 120 x 126464 x 4096 124.6 -> 120.4; with two row tiles or splits it costs
 // (376 x 12288 x 4096 28.9 -> 31.9, 120 x 4096 x 12288 20.9 -> 23.5).
+// Bound by the weight stream and the ramp at both ends: 120 x 24576 x 4096 25.3 us, 101 MB
+// of weights at 4.0 TB/s (4 slots a K-step 30.0 us; weights straight into registers, rows
+// through LDS, one barrier a K-step 31.7); 240 x 4096 x 12288 in 4 splits 20 us and 5 for
+// their sum; 1127 x 3584 x 18944 by its products, 85 us, 1800 TOP/s.
 template <int BM, int BN, int WM, int WN, int R>
 __global__ void __launch_bounds__(512, 2) gemm_i8_ks_kernel(const int8_t* __restrict__ A,
                                                             const int8_t* __restrict__ W, int K, int mt,
