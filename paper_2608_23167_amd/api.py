@@ -201,16 +201,28 @@ def _shape(t: torch.Tensor, shape, name: str) -> None:
         raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
 
 
-def _ws(ws: Optional[torch.Tensor]) -> Tuple[C.c_void_p, int]:
-    return (C.c_void_p(None), 0) if ws is None else (_ptr(ws, None, "ws"), ws.numel() * ws.element_size())
+def _arg(t: Optional[torch.Tensor], dtype, name: str) -> Optional[int]:
+    """_ptr as a plain number (None: NULL), which ctypes takes as well: calls of a
+    few us are bound by their arguments' checks."""
+    if t is None:
+        return None
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    return t.data_ptr()
 
 
-def _on_current(*tensors: Optional[torch.Tensor]) -> None:
-    """The library launches on the current device: tensors of another are refused."""
+def _on(stream, *tensors: Optional[torch.Tensor]) -> int:
+    """The stream's handle.  The library launches on the current device: tensors of
+    another are refused."""
     dev = torch.cuda.current_device()
     for t in tensors:
-        if t is not None and t.is_cuda and t.get_device() != dev:
+        if t is not None and t.get_device() != dev:
             raise ValueError(f"tensors must be on the current device (cuda:{dev}), got {t.device}")
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
 
 def ssm_norm_i8(x: torch.Tensor, gain: torch.Tensor, eps: float, q: torch.Tensor,
@@ -228,12 +240,12 @@ def ssm_norm_i8(x: torch.Tensor, gain: torch.Tensor, eps: float, q: torch.Tensor
         _shape(delta, (rows, d), "delta")
     if resid is not None:
         _shape(resid, (rows, d), "resid")
-    args = (rows, d, _ptr(x, torch.float32, "x"), _ptr(delta, None, "delta"),
-            0 if delta is None else _dt(delta, "delta"), _ptr(gain, None, "gain"),
-            _dt(gain, "gain"), float(eps), _ptr(resid, torch.float32, "resid"),
-            _ptr(q, torch.int8, "q"), _ptr(scale, torch.float32, "scale"))
-    _on_current(x, gain, q, scale, delta, resid)
-    check(lib().ssm_norm_i8(*args, _stream(stream)), "ssm_norm_i8")
+    args = (rows, d, _arg(x, torch.float32, "x"), _arg(delta, None, "delta"),
+            0 if delta is None else _dt(delta, "delta"), _arg(gain, None, "gain"),
+            _dt(gain, "gain"), float(eps), _arg(resid, torch.float32, "resid"),
+            _arg(q, torch.int8, "q"), _arg(scale, torch.float32, "scale"))
+    st = _on(stream, x, gain, q, scale, delta, resid)
+    check(lib().ssm_norm_i8(*args, st), "ssm_norm_i8")
 
 
 def ssm_quant_i8(x: torch.Tensor, q: torch.Tensor, scale: torch.Tensor, swiglu: bool = False,
@@ -244,10 +256,10 @@ def ssm_quant_i8(x: torch.Tensor, q: torch.Tensor, scale: torch.Tensor, swiglu: 
     rows, d = q.shape
     _shape(x, (rows, 2 * d if swiglu else d), "x")
     _shape(scale, (rows,), "scale")
-    args = (rows, d, int(bool(swiglu)), _dt(x, "x"), _ptr(x, None, "x"), _ptr(q, torch.int8, "q"),
-            _ptr(scale, torch.float32, "scale"))
-    _on_current(x, q, scale)
-    check(lib().ssm_quant_i8(*args, _stream(stream)), "ssm_quant_i8")
+    args = (rows, d, int(bool(swiglu)), _dt(x, "x"), _arg(x, None, "x"), _arg(q, torch.int8, "q"),
+            _arg(scale, torch.float32, "scale"))
+    st = _on(stream, x, q, scale)
+    check(lib().ssm_quant_i8(*args, st), "ssm_quant_i8")
 
 
 def ssm_gemm_i8_workspace_size(m: int, n: int, k: int) -> int:
@@ -266,11 +278,12 @@ def ssm_gemm_i8(a: torch.Tensor, a_scale: torch.Tensor, w: torch.Tensor, w_scale
     _shape(a_scale, (m,), "a_scale")
     _shape(w_scale, (n,), "w_scale")
     _shape(out, (m, n), "out")
-    args = (m, n, k, _ptr(a, torch.int8, "a"), _ptr(a_scale, torch.float32, "a_scale"),
-            _ptr(w, torch.int8, "w"), _ptr(w_scale, torch.float32, "w_scale"), _dt(out, "out"),
-            _ptr(out, None, "out"), *_ws(ws))
-    _on_current(a, a_scale, w, w_scale, out, ws)
-    check(lib().ssm_gemm_i8(*args, _stream(stream)), "ssm_gemm_i8")
+    args = (m, n, k, _arg(a, torch.int8, "a"), _arg(a_scale, torch.float32, "a_scale"),
+            _arg(w, torch.int8, "w"), _arg(w_scale, torch.float32, "w_scale"), _dt(out, "out"),
+            _arg(out, None, "out"), _arg(ws, None, "ws"),
+            0 if ws is None else ws.numel() * ws.element_size())
+    st = _on(stream, a, a_scale, w, w_scale, out, ws)
+    check(lib().ssm_gemm_i8(*args, st), "ssm_gemm_i8")
 
 
 def ssm_token_logprobs_workspace_size(rows: int, vocab: int, k: int) -> int:
@@ -295,6 +308,8 @@ def ssm_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor], ma
         raise ValueError("targets and logprob go together")
     t = 0
     if targets is not None:
+        if targets.dim() != 2:
+            raise ValueError(f"targets must be [{rows}, T], got {list(targets.shape)}")
         t = targets.shape[1]
         _shape(targets, (rows, t), "targets")
         _shape(logprob, (rows, t), "logprob")
@@ -305,12 +320,13 @@ def ssm_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor], ma
             raise ValueError("k > 0 needs top_ids and top_logprob")
         _shape(top_ids, (rows, k), "top_ids")
         _shape(top_logprob, (rows, k), "top_logprob")
-    args = (rows, vocab, _dt(logits, "logits"), _ptr(logits, None, "logits"), int(mask_id), t,
-            _ptr(targets, torch.int32, "targets"), int(k), _ptr(logprob, torch.float32, "logprob"),
-            _ptr(entropy, torch.float32, "entropy"), _ptr(top_ids, torch.int32, "top_ids"),
-            _ptr(top_logprob, torch.float32, "top_logprob"), *_ws(ws))
-    _on_current(logits, targets, logprob, entropy, top_ids, top_logprob, ws)
-    check(lib().ssm_token_logprobs(*args, _stream(stream)), "ssm_token_logprobs")
+    args = (rows, vocab, _dt(logits, "logits"), _arg(logits, None, "logits"), int(mask_id), t,
+            _arg(targets, torch.int32, "targets"), int(k), _arg(logprob, torch.float32, "logprob"),
+            _arg(entropy, torch.float32, "entropy"), _arg(top_ids, torch.int32, "top_ids"),
+            _arg(top_logprob, torch.float32, "top_logprob"), _arg(ws, None, "ws"),
+            0 if ws is None else ws.numel() * ws.element_size())
+    st = _on(stream, logits, targets, logprob, entropy, top_ids, top_logprob, ws)
+    check(lib().ssm_token_logprobs(*args, st), "ssm_token_logprobs")
 
 
 def ssm_unmask(tokens: torch.Tensor, block_start: int, block_size: int, mask_id: int, rule: int,

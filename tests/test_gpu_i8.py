@@ -70,7 +70,7 @@ def _gemm(a, sa, w, sw, dtype, ws_extra=0):
 # ---- norm ---------------------------------------------------------------------
 @pytest.mark.parametrize("rows,d", [(1, 1), (1, 4096), (3, 127), (5, 128), (17, 1000), (33, 512),
                                     (129, 3584), (7, 4096), (2, 8192), (3, 8196), (2, 20000),
-                                    (300, 4095)])
+                                    (300, 4095), (2, 8191), (2, 20001), (3, 33001), (2, 40000)])
 @pytest.mark.parametrize("delta", [None, F32, BF16, F16])
 def test_norm(gpu, rows, d, delta):
     gain = _rand(3, d, std=0.2, dtype=BF16 if rows % 2 else F32) + 1
@@ -110,7 +110,7 @@ def test_norm_unaligned(gpu, d, shift):
     R.check_codes(q, s, R.norm(r, gain, 1e-6), R.norm_rel(d))
 
 
-@pytest.mark.parametrize("d", [640, 4096, 4099])
+@pytest.mark.parametrize("d", [640, 4096, 4099, 33000])
 def test_norm_special_rows(gpu, d):
     x = _rand(1, 6, d)
     x[0] = 0
@@ -138,7 +138,7 @@ def test_norm_without_eps(gpu):
 
 # ---- rows to codes --------------------------------------------------------------
 @pytest.mark.parametrize("rows,d", [(1, 1), (1, 12288), (3, 127), (5, 128), (17, 1000), (240, 512),
-                                    (7, 3584), (2, 18944), (3, 20001), (2, 40000)])
+                                    (7, 3584), (3, 6000), (2, 18944), (3, 20001), (2, 40000), (1, 40003)])
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
 @pytest.mark.parametrize("swiglu", [False, True])
 def test_quant(gpu, rows, d, dtype, swiglu):
@@ -159,7 +159,7 @@ def test_quant_unaligned(gpu, d, shift, dtype, swiglu):
     R.check_codes(q, s, R.swiglu(x, d) if swiglu else x.double(), R.SWIGLU_REL if swiglu else 0.0)
 
 
-@pytest.mark.parametrize("d", [96, 3584, 20000])
+@pytest.mark.parametrize("d", [96, 3584, 20000, 33000])
 def test_quant_special_rows(gpu, d):
     x = torch.zeros(8, d, device=DEV)
     x[1] = 1e-39                                   # denormals: zero, scale 0
