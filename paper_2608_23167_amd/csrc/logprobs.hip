@@ -35,12 +35,6 @@ __device__ __forceinline__ void soft_move(Soft& a, float m) {     // to the maxi
   a.z *= e;
   a.m = m;
 }
-__device__ __forceinline__ Soft soft_join(Soft a, Soft b) {
-  const float M = max_nan(a.m, b.m);
-  soft_move(a, M);
-  soft_move(b, M);
-  return {M, a.z + b.z, a.t + b.t};
-}
 // Reductions over a wave by data-parallel moves (about 60 clocks; six shuffles
 // through LDS hardware take six times that): rows of 16 lanes, then across
 // rows, the total in lane 63 and from there, uniform, to all.
@@ -257,9 +251,7 @@ __global__ void __launch_bounds__(64 * NW) logprobs_kernel(
   if (lane < STAT_K) { sh[wave].v[lane] = bv; sh[wave].id[lane] = bi; }
   __syncthreads();
   if (wave != 0) return;
-  s = sh[0].s;
-#pragma unroll
-  for (int w = 1; w < NW; ++w) s = soft_join(s, sh[w].s);
+  s = soft_wave(lane < NW ? sh[lane].s : Soft{-INFINITY, 0.f, 0.f});
   auto next = [&](int j, float& v, int& i) {
     v = lane < NW ? sh[lane].v[j] : -INFINITY;
     i = lane < NW ? sh[lane].id[j] : STAT_NONE;
@@ -294,21 +286,29 @@ __global__ void __launch_bounds__(64) logprobs_join_kernel(
   });
 }
 
-// Parts of a row: 768 workgroups, 3 to a CU, in parts of at least a tile to each wave.
-// Rows in parts cost a second launch (4 us) but fill the card: 120 rows of 126464
-// float32 logits in 6 parts 23.9 us (8 parts 23.5), 240 rows in 3 parts 31.3; 400 rows
-// whole 43.4, in 2 parts 46.9.
+// Waves of a workgroup, and parts of a row.
+//  * Up to 2048 columns a wave takes a row (at most two tiles).
+//  * Up to 256 rows, a workgroup of 16 waves on each CU takes a whole row where that is
+//    sooner than parts: 6 us + 0.113 us a thousand columns against 9.5 us (two launches) +
+//    0.68 us a million of all rows' columns.  Measured, float32: one row of 16384 8.0
+//    against 10.5 us, of 65536 14.9 against 10.7; 120 rows of 32768 12.8 against 14.7;
+//    240 rows of 126464 27.6 against 31.6.
+//  * Else workgroups of 4 waves; whole rows once there are 385, below in parts of at least a
+//    tile to each wave, 768 workgroups, 3 to a CU: 120 rows of 126464 in 6 parts 23.9 us, in
+//    8 23.5; 400 rows whole 43.4, in 2 parts 46.9.
 struct LogprobsPlan {
-  int parts, chunk;
+  int waves, parts, chunk;
 };
 static LogprobsPlan logprobs_plan(int rows, int V) {
-  constexpr int LEAST = 4096, WORKGROUPS = 768;
+  constexpr int LEAST = 4096, WORKGROUPS = 768, CUS = 256;
+  if (V <= 2048) return {1, 1, V};
+  if (V > LEAST && rows <= CUS && V * (113.0 - 0.68 * rows) < 3.5e6) return {16, 1, V};
   int parts = WORKGROUPS / rows;
   if (parts > V / LEAST) parts = V / LEAST;
   if (parts > 64) parts = 64;
-  if (parts <= 1) return {1, V};
+  if (parts <= 1) return {4, 1, V};
   const int chunk = ceil_div(ceil_div(V, parts), LEAST) * LEAST;
-  return {ceil_div(V, chunk), chunk};
+  return {4, ceil_div(V, chunk), chunk};
 }
 
 size_t token_logprobs_ws_bytes(int rows, int V, int k) {
@@ -327,12 +327,13 @@ hipError_t launch_token_logprobs(int dtype, int rows, int V, const void* logits,
   Part* part = (Part*)ws;
   auto go = [&](auto* x) {
     using T = std::remove_cv_t<std::remove_pointer_t<decltype(x)>>;
-    if (V <= 2048)                                  // at most two tiles: a wave to a row
-      launch((logprobs_kernel<T, 1>), dim3(rows), dim3(64), 0, st, x, V, mask_id, n_targets, targets,
-             k, 1, V, lp, entropy, top_ids, top_lp, part);
-    else
-      launch((logprobs_kernel<T, 4>), dim3(rows * p.parts), dim3(256), 0, st, x, V, mask_id, n_targets,
-             targets, k, p.parts, p.chunk, lp, entropy, top_ids, top_lp, part);
+    const auto rows_by = [&](auto kernel) {
+      launch(kernel, dim3(rows * p.parts), dim3(64 * p.waves), 0, st, x, V, mask_id, n_targets, targets, k,
+             p.parts, p.chunk, lp, entropy, top_ids, top_lp, part);
+    };
+    if (p.waves == 1) rows_by(logprobs_kernel<T, 1>);
+    else if (p.waves == 16) rows_by(logprobs_kernel<T, 16>);
+    else rows_by(logprobs_kernel<T, 4>);
     if (p.parts > 1)
       launch(logprobs_join_kernel<T>, dim3(rows), dim3(64), 0, st, part, p.parts, x, V, mask_id,
              n_targets, targets, k, lp, entropy, top_ids, top_lp);

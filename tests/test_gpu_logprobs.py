@@ -75,7 +75,7 @@ def _ids(seed, rows, t, vocab):
 
 @pytest.mark.parametrize("rows,vocab", [(1, 1), (1, 2), (3, 7), (2, 63), (5, 64), (4, 257), (33, 512), (1, 4097),
                                         (7, 8191), (130, 1000), (1, 126464), (3, 152064), (40, 30001),
-                                        (600, 2050), (2, 300007)])
+                                        (600, 2050), (2, 300007), (150, 60001), (2, 16384), (300, 8200)])
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
 def test_scores(gpu, rows, vocab, dtype):
     x = _logits(rows + vocab, rows, vocab, dtype)
