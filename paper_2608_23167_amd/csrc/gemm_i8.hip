@@ -9,7 +9,6 @@
 // operand, and a lane then holds 4 consecutive outputs of one row.
 #include <stdio.h>
 #include <stdlib.h>
-#include <string.h>
 
 #include "internal.h"
 #include "tiles.h"
@@ -516,8 +515,8 @@ __global__ void __launch_bounds__(512, 2) gemm_i8_pp_kernel(const int8_t* __rest
 // (376 x 12288 x 4096 28.9 -> 31.9, 120 x 4096 x 12288 20.9 -> 23.5).
 // Bound by the weight stream and the ramp at both ends: 120 x 24576 x 4096 25.3 us, 101 MB
 // of weights at 4.0 TB/s (4 slots a K-step 30.0 us; weights straight into registers, rows
-// through LDS, one barrier a K-step 31.7); 240 x 4096 x 12288 in 4 splits 20 us and 5 for
-// their sum; 1127 x 3584 x 18944 by its products, 85 us, 1800 TOP/s.
+// through LDS, one barrier a K-step 31.7); 240 x 4096 x 12288 in 4 splits 20 us and 4.4
+// for their sum; 1127 x 3584 x 18944 by its products, 85 us, 1800 TOP/s.
 template <int BM, int BN, int WM, int WN, int R>
 __global__ void __launch_bounds__(512, 2) gemm_i8_ks_kernel(const int8_t* __restrict__ A,
                                                             const int8_t* __restrict__ W, int K, int mt,
@@ -680,19 +679,24 @@ __global__ void __launch_bounds__(512, 2) gemm_i8_ks_kernel(const int8_t* __rest
 // ---------------------------------------------------------------------------
 // Sum of split-K partials
 // ---------------------------------------------------------------------------
-// 4 columns a thread; part is [S, M, ldp] with ldp a multiple of 16.
-__global__ void __launch_bounds__(256) gemm_i8_sum_kernel(const int* __restrict__ part, int S, int ldp,
-                                                          I8Out out) {
-  const int M = out.M;
-  const size_t x = (size_t)blockIdx.x * 256 + threadIdx.x, per = ldp >> 2;
-  if (x >= (size_t)M * per) return;
-  const int m = (int)(x / per), n = 4 * (int)(x % per);
+// 4 columns a thread, a row to a workgroup (or several, a grid apart); part is [S, M,
+// ldp] with ldp a multiple of 16.  The S loads of a thread are in flight together.
+template <int S>
+__global__ void __launch_bounds__(256) gemm_i8_sum_kernel(const int* __restrict__ part, int ldp, I8Out out) {
+  const int n = 4 * (int)(blockIdx.x * 256 + threadIdx.x);
   if (n >= out.N) return;
-  i32x4_t sum = {0, 0, 0, 0};
-  for (int v = 0; v < S; ++v) sum += *(const i32x4_t*)(part + ((size_t)v * M + m) * ldp + n);
   float s[4];
   out.scales4(n, s);
-  out.store4(m, n, sum, out.sa[m], s);
+  for (int m = blockIdx.y; m < out.M; m += gridDim.y) {
+    i32x4_t v[S];
+#pragma unroll
+    for (int i = 0; i < S; ++i) v[i] = *(const i32x4_t*)(part + ((size_t)i * out.M + m) * ldp + n);
+    const float sm = out.sa[m];
+    i32x4_t sum = v[0];
+#pragma unroll
+    for (int i = 1; i < S; ++i) sum += v[i];
+    out.store4(m, n, sum, sm, s);
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -733,6 +737,7 @@ static constexpr I8Tile I8_TILE[] = {
 #undef X
 };
 static constexpr int I8_CUS = 256;
+static constexpr int I8_SPLITS[] = {1, 2, 3, 4, 6, 8};
 static constexpr float I8_HBM = 6.5e6f;          // bytes a us
 static constexpr float I8_SUM_BYTES = 5.0e6f;    // of partials written and read again, a us
 static constexpr float I8_SUM_US = 1.9f;         // the launch that adds them
@@ -771,7 +776,7 @@ static I8Plan i8_plan(int M, int N, int K) {
   float least = M <= I8_FEW_ROWS ? i8_few_cost(M, N, K) : 1e30f;
   if (K < 128) return best;                        // the tiles need a whole K-step
   for (int i = 0; i < (int)(sizeof(I8_TILE) / sizeof(I8_TILE[0])); ++i)
-    for (int S : {1, 2, 3, 4, 6, 8}) {
+    for (int S : I8_SPLITS) {
       if (S > 1 && K / 128 / S < 4) break;
       const float us = i8_cost(I8_TILE[i], M, N, K, S);
       if (us < least) {
@@ -819,8 +824,16 @@ hipError_t gemm_i8(int M, int N, int K, const int8_t* a, const float* sa, const 
       launch(gemm_i8_few_kernel<4>, dim3(ceil_div(N, 16)), dim3(512), 0, st, a, w, K, o);
   }
   if (part) {
-    const size_t n = (size_t)M * (i8_ldp(N) / 4);
-    launch(gemm_i8_sum_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, part, p.split, i8_ldp(N), o);
+    const auto add = [&](auto kernel) {
+      launch(kernel, dim3(ceil_div(N, 1024), M < 65535 ? M : 65535), dim3(256), 0, st, part, i8_ldp(N), o);
+    };
+    switch (p.split) {                             // I8_SPLITS
+      case 2: add(gemm_i8_sum_kernel<2>); break;
+      case 3: add(gemm_i8_sum_kernel<3>); break;
+      case 4: add(gemm_i8_sum_kernel<4>); break;
+      case 6: add(gemm_i8_sum_kernel<6>); break;
+      default: add(gemm_i8_sum_kernel<8>); break;
+    }
   }
   return hipGetLastError();
 }
