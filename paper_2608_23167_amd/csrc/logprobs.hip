@@ -141,7 +141,9 @@ __device__ __forceinline__ void row_results(size_t row, const Soft& s, const T* 
 // no order happens k ln(tiles) times a wave.  Where more than k lanes are above
 // it, as in the first tile or in rising rows, the k-th largest of the lanes'
 // maxima is a floor for this tile's candidates.  Each candidate then goes to its
-// place in the list by value and id.
+// place in the list by value and id; one that finds none takes along all that
+// are no better than the k-th (3840 rows of 126464 bfloat16 logits, k = 8: random 217 us,
+// all equal 180, without this 867; rising 920, without 3637).
 template <typename T, int NW>
 __global__ void __launch_bounds__(64 * NW) logprobs_kernel(
     const T* __restrict__ logits, int V, int mask_id, int n_targets,
@@ -206,6 +208,12 @@ __global__ void __launch_bounds__(64 * NW) logprobs_kernel(
         const float v = lane_of(x[e], l);
         const int id = base + l * step + off(e);
         const int place = __popcll(__ballot(lane < k && stat_better(bv, bi, v, id)));
+        if (place >= k) {                          // with it go all that are no better than the k-th
+          const float kv = lane_of(bv, k - 1);
+          const int ki = __builtin_amdgcn_readlane(bi, k - 1);
+          found &= __ballot(stat_better(x[e], base + lane * step + off(e), kv, ki));
+          continue;
+        }
         const float uv = __int_as_float(from_below(__float_as_int(bv)));
         const int ui = from_below(bi);
         if (lane == place) { bv = v; bi = id; }
