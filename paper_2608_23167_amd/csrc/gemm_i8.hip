@@ -500,24 +500,32 @@ __global__ void __launch_bounds__(512, 2) gemm_i8_pp_kernel(const int8_t* __rest
 // The alternation above for smaller tiles, where a phase's LDS reads and its
 // barriers would outlast its MFMAs: the waves 0-3 take half 0 of every K-step of
 // 128 and the waves 4-7 half 1, each group the whole BM x BN tile (WM x WN = 4
-// waves), so a wave has a tile twice as large, reads less for each MFMA, and a
-// K-step has 2 slots instead of 4.  The groups' sums join in LDS at the end.
-// Slot 2t: the first group reads half 0 of K-step t while the second multiplies
-// half 1 of t - 1; slot 2t + 1: the other way round.  Rows and weights share a
-// ring of R stages; a wave's copies of K-step t + R - 1, begun in its memory part
-// of t, overwrite the stage of t - 1, read last in slot 2t - 1.  Before the
-// barrier that opens slot 2t + 2 each wave waits until only its copies of the
-// R - 2 latest K-steps are in flight: those of t + 1 have then landed.  All
-// copies are whole lines (8 rows of 128 bytes, chunks placed as above).  Weights that
-// one workgroup reads (a single row tile, K not split) are loaded nontemporal, which
-// leaves the caches to the rows: 120 x 24576 x 4096 29.5 -> 27.7 us, 40 rows 21.6 ->
-// 20.1, 120 x 126464 x 4096 124.6 -> 120.4; with two row tiles or splits it costs
-// (376 x 12288 x 4096 28.9 -> 31.9, 120 x 4096 x 12288 20.9 -> 23.5).
-// Bound by the weight stream and the ramp at both ends: 120 x 24576 x 4096 25.3 us, 101 MB
-// of weights at 4.0 TB/s (4 slots a K-step 30.0 us; weights straight into registers, rows
-// through LDS, one barrier a K-step 31.7); 240 x 4096 x 12288 in 4 splits 20 us and 4.4
-// for their sum; 1127 x 3584 x 18944 by its products, 85 us, 1800 TOP/s.
-template <int BM, int BN, int WM, int WN, int R>
+// waves), so a wave has a tile twice as large and reads less for each MFMA, and a
+// K-step takes 1 or 2 barriers instead of 4.  The groups' sums join in LDS at the end.
+// Rows and weights share a ring of R stages; all copies are whole lines (8 rows of
+// 128 bytes, chunks placed as above).
+//  * In alternation (AHEAD false): slot 2t, the first group reads half 0 of K-step t
+//    while the second multiplies half 1 of t - 1; slot 2t + 1, the other way round.  A
+//    wave's copies of K-step t + R - 1, begun in its memory part of t, overwrite the stage
+//    of t - 1, read last in slot 2t - 1.  Before the barrier that opens slot 2t + 2 each
+//    wave waits until only its copies of the R - 2 latest K-steps are in flight: those of
+//    t + 1 have then landed.
+//  * Both groups at once (AHEAD true, tiles up to 128 x 96, whose MFMAs are shorter than a
+//    trip to LDS): in K-step t a wave reads its operands of t + 1 into a second set of
+//    registers, begins its copies of t + R into the stage of t (read in t - 1), multiplies
+//    K-step t, and waits as above, so that t + 2 has landed; one barrier.  120 x 4096 x 4096
+//    on 64 x 32 tiles 12.1 -> 10.6 us, 240 x 4096 x 4096 on 64 x 64 14.1 -> 13.1, 120 x 24576 x
+//    4096 on 128 x 96 26.7 -> 25.5; 128 x 192 34.7 -> 35.3, 256 x 128 spills (83 -> 90).
+// Weights that one workgroup reads (a single row tile, K not split) are loaded
+// nontemporal, which leaves the caches to the rows: 120 x 24576 x 4096 29.5 -> 27.7 us, 40
+// rows 21.6 -> 20.1, 120 x 126464 x 4096 124.6 -> 120.4; with two row tiles or splits it
+// costs (376 x 12288 x 4096 28.9 -> 31.9, 120 x 4096 x 12288 20.9 -> 23.5).
+// Bound by the weight stream and the ramp at both ends: 120 x 24576 x 4096 25.0 us, 101 MB
+// of weights at 4.0 TB/s (gemm_i8_pp_kernel on the same tile 30.0 us; weights straight into
+// registers, rows through LDS, one barrier a K-step 31.7); 240 x 4096 x 12288 in 4 splits
+// 20 us and 4.4 for their sum; 1127 x 3584 x 18944 by LDS (64 KB read and 32 written a K-step,
+// 768 clocks at its rate, for 512 of MFMAs), 85 us, 1800 TOP/s.
+template <int BM, int BN, int WM, int WN, int R, bool AHEAD>
 __global__ void __launch_bounds__(512, 2) gemm_i8_ks_kernel(const int8_t* __restrict__ A,
                                                             const int8_t* __restrict__ W, int K, int mt,
                                                             int n_split, int* __restrict__ part,
@@ -591,25 +599,30 @@ __global__ void __launch_bounds__(512, 2) gemm_i8_ks_kernel(const int8_t* __rest
   for (int i = 0; i < FM; ++i)
 #pragma unroll
     for (int j = 0; j < FN; ++j) acc[i][j] = i32x4_t{0, 0, 0, 0};
-  i32x4_t af[FM], wf[FN];
+  i32x4_t af[AHEAD ? 2 : 1][FM], wf[AHEAD ? 2 : 1][FN];
 
   const int r16 = lane & 15, g4 = lane >> 4;
   const int frag = r16 * 128 + (((g4 ^ (r16 >> 1)) << 4) ^ (late ? 64 : 0));   // this group's half
-  auto read = [&](int stage) {
+  auto read = [&](int stage, i32x4_t (&ar)[FM], i32x4_t (&wr)[FN]) {
     const char* a = smem + stage * STAGE + wm * RW * 128 + frag;
     const char* w = smem + stage * STAGE + BM * 128 + wn * CW * 128 + frag;
 #pragma unroll
-    for (int j = 0; j < FN; ++j) wf[j] = *(const i32x4_t*)(w + j * 2048);
+    for (int j = 0; j < FN; ++j) wr[j] = *(const i32x4_t*)(w + j * 2048);
 #pragma unroll
-    for (int i = 0; i < FM; ++i) af[i] = *(const i32x4_t*)(a + i * 2048);
+    for (int i = 0; i < FM; ++i) ar[i] = *(const i32x4_t*)(a + i * 2048);
   };
-  auto mma = [&]() {
+  auto mma = [&](const i32x4_t (&ar)[FM], const i32x4_t (&wr)[FN]) {
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
-      for (int j = 0; j < FN; ++j) acc[i][j] = mma_i8(wf[j], af[i], acc[i][j]);
+      for (int j = 0; j < FN; ++j) acc[i][j] = mma_i8(wr[j], ar[i], acc[i][j]);
     __builtin_amdgcn_s_setprio(0);
+  };
+  auto wait_reads = [] { __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14)); };   // lgkmcnt(0)
+  auto wait_copies = [&] {
+    if (late) wait_vmcnt<FLIGHT1>();
+    else wait_vmcnt<FLIGHT0>();
   };
 
   // the groups share the epilogue: the first keeps the fragments i < FM / 2, the
@@ -618,27 +631,48 @@ __global__ void __launch_bounds__(512, 2) gemm_i8_ks_kernel(const int8_t* __rest
   TileScales<H, FN> sc;
   if (!part) sc.load(out, m0 + wm * RW + (late ? 16 * H : 0) + r16, n0 + wn * CW + 4 * g4);
 #pragma unroll
-  for (int j = 0; j < R - 1; ++j) issue(j, j);
-  if (late) wait_vmcnt<FLIGHT1>();
-  else wait_vmcnt<FLIGHT0>();
+  for (int j = 0; j < (AHEAD ? R : R - 1); ++j) issue(j, j);
+  wait_copies();
   if (!part) sc.hold();
   pp_barrier();
-  if (late) pp_barrier();
   int st = 0;                                       // stage of K-step v
-  for (int v = 0; v < nk; ++v) {
-    read(st);
-    issue(v + R - 1, st == 0 ? R - 1 : st - 1);
-    __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));   // lgkmcnt(0)
-    if (late) wait_vmcnt<FLIGHT1>();
+  if constexpr (AHEAD) {
+    read(0, af[0], wf[0]);
+    wait_reads();
     pp_barrier();
-    mma();
-    __builtin_amdgcn_sched_barrier(0);
-    if (!late) wait_vmcnt<FLIGHT0>();
-    pp_barrier();
-    st = st == R - 1 ? 0 : st + 1;
+    auto step = [&](int v, int now) {
+      const int next = st == R - 1 ? 0 : st + 1;
+      read(next, af[now ^ 1], wf[now ^ 1]);
+      issue(v + R, st);
+      __builtin_amdgcn_sched_barrier(0);
+      mma(af[now], wf[now]);
+      __builtin_amdgcn_sched_barrier(0);
+      wait_reads();
+      wait_copies();
+      pp_barrier();
+      st = next;
+    };
+    for (int v = 0; v < nk; v += 2) {
+      step(v, 0);
+      if (v + 1 < nk) step(v + 1, 1);
+    }
+  } else {
+    if (late) pp_barrier();
+    for (int v = 0; v < nk; ++v) {
+      read(st, af[0], wf[0]);
+      issue(v + R - 1, st == 0 ? R - 1 : st - 1);
+      __builtin_amdgcn_sched_barrier(0);
+      wait_reads();
+      if (late) wait_vmcnt<FLIGHT1>();
+      pp_barrier();
+      mma(af[0], wf[0]);
+      __builtin_amdgcn_sched_barrier(0);
+      if (!late) wait_vmcnt<FLIGHT0>();
+      pp_barrier();
+      st = st == R - 1 ? 0 : st + 1;
+    }
+    if (!late) pp_barrier();
   }
-  if (!late) pp_barrier();
   wait_vmcnt<0>();                                  // no copy lands in the sums below
 
   if ((K & 127) && split == n_split - 1) {          // the columns past the last whole K-step
@@ -647,13 +681,13 @@ __global__ void __launch_bounds__(512, 2) gemm_i8_ks_kernel(const int8_t* __rest
       const int k = k0 + 16 * g4, kc = min(k, K - 16);
 #pragma unroll
       for (int j = 0; j < FN; ++j)
-        wf[j] = *(const i32x4_t*)(W + (size_t)min(n0 + wn * CW + 16 * j + r16, N - 1) * K + kc);
+        wf[0][j] = *(const i32x4_t*)(W + (size_t)min(n0 + wn * CW + 16 * j + r16, N - 1) * K + kc);
 #pragma unroll
       for (int i = 0; i < FM; ++i) {
         const i32x4_t u = *(const i32x4_t*)(A + (size_t)min(m0 + wm * RW + 16 * i + r16, M - 1) * K + kc);
-        af[i] = k < K ? u : i32x4_t{0, 0, 0, 0};
+        af[0][i] = k < K ? u : i32x4_t{0, 0, 0, 0};
       }
-      mma();
+      mma(af[0], wf[0]);
     }
   }
 
@@ -708,8 +742,8 @@ __global__ void __launch_bounds__(256) gemm_i8_sum_kernel(const int* __restrict_
 // takes step + fill * w / 256 us, the second part for what the CUs share, but the
 // weights come no faster than I8_HBM bytes a us; `fixed` is what a round takes besides.
 // Measured on 160 sizes (40-3840 rows, 700-126464 columns, K 1024-18944) times 12
-// tiles times 6 splits, the weights from memory: the choice takes 0.8% more than
-// the best of them in the mean, 11% at most.  The kernel for few rows took 7.3 us for
+// tiles times 6 splits, the weights from memory: the choice takes 0.4% more than
+// the best of them in the mean, 12% at most.  The kernel for few rows took 7.3 us for
 // one row of 4096 x 4096 (64 x 32 tiles 10.3), 12.5 of 4096 x 12288 (15.1), but 27.7 of
 // 24576 x 4096 (64 x 96 tiles 20.4), and for 16 rows 8.6, 17.4 and 38.6 (10.1, 15.5, 20.8).
 static constexpr int I8_FEW_ROWS = 16;
@@ -720,17 +754,17 @@ struct I8Tile {
 // number, gemm_i8_pp_kernel (1) or gemm_i8_ks_kernel (0), BM, BN, WM, WN, stages; step, fill, fixed
 #define I8_TILES(X)                              \
   X(0, 0, 64, 32, 2, 2, 8, 0.18f, 0.02f, 1.9f)   \
-  X(1, 0, 64, 64, 2, 2, 8, 0.24f, 0.03f, 2.4f)   \
-  X(2, 0, 64, 96, 2, 2, 8, 0.24f, 0.07f, 2.9f)   \
+  X(1, 0, 64, 64, 2, 2, 8, 0.24f, 0.03f, 2.0f)   \
+  X(2, 0, 64, 96, 2, 2, 8, 0.24f, 0.07f, 4.1f)   \
   X(3, 0, 128, 64, 2, 2, 6, 0.29f, 0.10f, 2.4f)  \
-  X(4, 0, 128, 96, 2, 2, 5, 0.30f, 0.17f, 3.0f)  \
-  X(5, 0, 128, 128, 2, 2, 5, 0.34f, 0.20f, 3.3f) \
-  X(6, 0, 128, 160, 2, 2, 4, 0.42f, 0.23f, 3.7f) \
-  X(7, 0, 128, 192, 2, 2, 4, 0.44f, 0.28f, 4.3f) \
+  X(4, 0, 128, 96, 2, 2, 5, 0.35f, 0.20f, 3.0f)  \
+  X(5, 0, 128, 128, 2, 2, 5, 0.34f, 0.27f, 3.3f) \
+  X(6, 0, 128, 160, 2, 2, 4, 0.46f, 0.23f, 3.7f) \
+  X(7, 0, 128, 192, 2, 2, 4, 0.44f, 0.30f, 4.3f) \
   X(8, 0, 256, 128, 2, 2, 3, 0.54f, 0.32f, 3.4f) \
   X(9, 1, 128, 256, 2, 4, 2, 0.93f, 0.19f, 2.9f) \
-  X(10, 1, 256, 192, 4, 2, 2, 0.76f, 0.66f, 1.5f) \
-  X(11, 1, 256, 256, 2, 4, 2, 0.88f, 0.55f, 9.4f)
+  X(10, 1, 256, 192, 4, 2, 2, 0.76f, 0.60f, 1.5f) \
+  X(11, 1, 256, 256, 2, 4, 2, 0.84f, 0.55f, 9.2f)
 static constexpr I8Tile I8_TILE[] = {
 #define X(I, PP, BM, BN, WM, WN, R, STEP, FILL, FIXED) {BM, BN, STEP, FILL, FIXED},
     I8_TILES(X)
@@ -740,7 +774,7 @@ static constexpr int I8_CUS = 256;
 static constexpr int I8_SPLITS[] = {1, 2, 3, 4, 6, 8};
 static constexpr float I8_HBM = 6.5e6f;          // bytes a us
 static constexpr float I8_SUM_BYTES = 5.0e6f;    // of partials written and read again, a us
-static constexpr float I8_SUM_US = 1.9f;         // the launch that adds them
+static constexpr float I8_SUM_US = 1.8f;         // the launch that adds them
 
 struct I8Plan {
   int tile, split;           // tile -1: gemm_i8_few_kernel
@@ -801,7 +835,8 @@ static void launch_tile(int split, int M, int N, int K, const int8_t* a, const i
   if constexpr (PP)
     launch((gemm_i8_pp_kernel<BM, BN, WM, WN, R>), grid, block, 0, st, a, w, K, mt, split, part, i8_ldp(N), out);
   else
-    launch((gemm_i8_ks_kernel<BM, BN, WM, WN, R>), grid, block, 0, st, a, w, K, mt, split, part, i8_ldp(N), out);
+    launch((gemm_i8_ks_kernel<BM, BN, WM, WN, R, (BM * BN <= 128 * 96)>), grid, block, 0, st, a, w, K, mt, split,
+           part, i8_ldp(N), out);
 }
 
 hipError_t gemm_i8(int M, int N, int K, const int8_t* a, const float* sa, const int8_t* w,

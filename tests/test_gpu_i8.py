@@ -196,7 +196,9 @@ TILE_SIZES = [(30, 1008, 352), (1101, 157, 3904), (1084, 129, 3088), (68, 186, 2
               (25, 126, 5696), (1382, 603, 320), (950, 2114, 320), (1033, 9943, 1360), (27, 18307, 416),
               (949, 1156, 336), (517, 3333, 576), (1064, 2780, 528), (2498, 1597, 784), (262, 14266, 1168),
               (2105, 2519, 816), (301, 21310, 944), (2379, 277, 5648), (641, 663, 6624), (885, 587, 4768),
-              (82, 1514, 4784), (79, 5656, 6160), (68, 8503, 6288)]
+              (82, 1514, 4784), (79, 5656, 6160), (68, 8503, 6288), (2894, 323, 4112), (2915, 1493, 912),
+              (412, 10959, 912), (262, 20255, 1392), (575, 16431, 1104), (2588, 1201, 672),
+              (1351, 155, 5696), (133, 2058, 6176)]
 
 
 @pytest.mark.parametrize("m,n,k", SIZES + TILE_SIZES)
