@@ -330,12 +330,28 @@ __global__ void __launch_bounds__(512) gemm_i8_few_kernel(const int8_t* __restri
 // 16-19 and 28-31) together, which counters say is how they go: with r / 4 for
 // half_place(r), even for the first grouping only, 13% of the clocks were conflicts.
 // What is left of K past the last whole K-step is multiplied from registers.
-// 3840 x 24576 x 4096: 361 us, 2140 TOP/s; the MFMAs are busy 53% of the clocks, and the
+// 3840 x 24576 x 4096: 356 us, 2170 TOP/s; the MFMAs are busy 53% of the clocks, and the
 // clock gives way to the power of that (1.9 GHz).  Of a round of 61 us 10 pass before the
 // first product and after the last; workgroups that stay for several tiles and start
 // the next one's copies before they store were tried: the loop around it all spilled.
 __device__ __forceinline__ int half_place(int r) {      // 0, 2, 3, 1 for r / 4 = 0 .. 3
   return ((r >> 2) & 1) * 2 ^ ((r >> 3) & 1) * 3;
+}
+
+// tile_of with the row tiles in groups of 4, innermost in a group: the 32 tiles that an XCD
+// works on at a time are then about 4 x 8 and need 12 strips of rows and weights in its
+// L2, where 15 x 2 need 17.  3840 x 24576 x 4096 371 -> 363 us, 3840 x 12288 x 4096 182 -> 174,
+// 14208 x 24576 x 4096 1297 -> 1222 (2340 TOP/s); groups of 8 368, 175 and 1273.
+__device__ __forceinline__ void grouped_tile_of(int w, int total, int ntm, int mt, int& split, int& tn,
+                                                int& tm) {
+  constexpr int GROUP = 4;
+  const int per = total / 8;
+  const int v = w < per * 8 ? (w % 8) * per + (w / 8) : w;
+  split = v / ntm;
+  const int x = v % ntm, nt = ntm / mt, first = x / (GROUP * nt) * GROUP, rows = min(GROUP, mt - first);
+  const int y = x - first * nt;
+  tm = first + y % rows;
+  tn = y / rows;
 }
 
 template <int BM, int BN, int WM, int WN, int PA>
@@ -359,7 +375,7 @@ __global__ void __launch_bounds__(512, 2) gemm_i8_pp_kernel(const int8_t* __rest
   const int wm = wave % WM, wn = wave / WM;
   const bool late = wave >= 4;                     // the second group
   int t, mtile, split;
-  tile_of(blockIdx.x, gridDim.x, gridDim.x / n_split, mt, split, t, mtile);
+  grouped_tile_of(blockIdx.x, gridDim.x, gridDim.x / n_split, mt, split, t, mtile);
   const int M = out.M, N = out.N, m0 = mtile * BM, n0 = t * BN;
   const int k_steps = K >> 7;                      // whole ones
   const int ks0 = (int)((long long)split * k_steps / n_split);
