@@ -381,9 +381,11 @@ int32_t ssm_gather_rows(int32_t batch, int32_t src_rows, int32_t width, const vo
  *   (SSM_DT_F32 or BF16); d_q int8 [rows, d]; d_scale float32 [rows];
  *   d_resid float32 [rows, d], or NULL; it may be d_x or a float32 d_delta
  *   itself (in place) but must not overlap them otherwise.
- * eps finite and >= 0.  Squares and r * gain are formed in float32: |r| stays
- * below 2^56, |r * gain| below 2^127, and with eps = 0 a row's root mean square
- * above 2^-60 (a row of zeros has no norm then: its scale is NaN).
+ * eps finite and >= 0.  Squares and r * gain are formed in float32: a row whose
+ * squares add up to 2^128 or more (none has |r| below 2^64 / sqrt(d)), or whose mean
+ * square plus eps does, gets scale NaN and codes 0; |r * gain| stays below 2^127.
+ * With eps = 0 a row's root mean square stays above 2^-60 and its largest |r * gain|
+ * above 2^-126 (a row of zeros has no norm then: its scale is NaN).
  */
 int32_t ssm_norm_i8(int32_t rows, int32_t d, const float* d_x, const void* d_delta,
                     int32_t delta_dtype, const void* d_gain, int32_t gain_dtype, float eps,

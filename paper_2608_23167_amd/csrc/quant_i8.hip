@@ -83,6 +83,13 @@ template <int V> __device__ __forceinline__ void store_codes(int8_t* q, const fl
   }
 }
 
+// 1 / sqrt(mean + eps) for a row's sum of squares; NaN, which makes the row's scale NaN,
+// where that sum has overflowed: 1 / sqrt(inf) = 0 would make a row of zeros of it.
+__device__ __forceinline__ float inverse_rms(float ss, int d, float eps) {
+  const float ms = ss / (float)d + eps;
+  return ms < INFINITY ? 1.0f / sqrtf(ms) : __uint_as_float(0x7fc00000u);
+}
+
 // Sum and largest bits over the TPR threads of a row.
 template <int TPR>
 __device__ __forceinline__ void row_reduce(float& s, uint32_t& a, float* red, uint32_t* redu) {
@@ -185,7 +192,7 @@ norm_rows_kernel(const float* x, const TD* delta, const TG* __restrict__ g, int 
     }
   }
   row_reduce<TPR>(ss, a, red, redu);
-  const float inv = 1.0f / sqrtf(ss / (float)d + eps);
+  const float inv = inverse_rms(ss, d, eps);
   const Codes k = codes_of(abs_bits(__uint_as_float(a) * inv));
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
@@ -240,7 +247,7 @@ __global__ void __launch_bounds__(256) norm_i8_kernel(const float* x, const TD* 
   float ss = 0.f;
   for (int c = threadIdx.x; c < d; c += 256) { const float r = sum(c); ss += r * r; }
   ss = block_sum256(ss, red);
-  const float inv = 1.0f / sqrtf(ss / (float)d + eps);
+  const float inv = inverse_rms(ss, d, eps);
   uint32_t a = 0;
   for (int c = threadIdx.x; c < d; c += 256) a = max(a, abs_bits(sum(c) * inv * ldf(g + c)));
   const Codes k = codes_of(block_max256(a, redu));
