@@ -406,8 +406,9 @@ int32_t ssm_gemm_i8_workspace_size(int32_t m, int32_t n, int32_t k, size_t* byte
  * d_out[i, j] = d_a_scale[i] * d_w_scale[j] * sum_l d_a[i, l] * d_w[j, l]
  * for int8 rows d_a [m, k], int8 weights d_w [n, k], float32 scales [m] and [n];
  * d_out [m, n] of out_dtype (SSM_DT_F32, BF16 or F16).  The sums are exact
- * int32 (any codes in [-128, 127]); the sum times the product of the two
- * scales is computed in float32 and rounded once to out_dtype.
+ * int32 (any codes in [-128, 127]); the sum times d_a_scale[i], and that times
+ * d_w_scale[j], are computed in float32 (|sum * d_a_scale[i]| stays below 2^128),
+ * and the result is rounded once to out_dtype.
  * k up to 131071 (SSM_E_UNSUPPORTED above); m = 0 launches nothing.  Rows are
  * read fastest where k is a multiple of 16 and d_a, d_w are 16-byte aligned.
  * d_ws: 16-byte aligned workspace of ws_bytes >= ssm_gemm_i8_workspace_size(m,

@@ -1,7 +1,7 @@
 // Products of 8-bit rows with 8-bit weights:
 //   out[m, n] = a_scale[m] * w_scale[n] * sum_k a[m, k] * w[n, k]
 // The sums are int32 and exact (K < 2^17), whatever the order; the two scales
-// are multiplied onto the sum in float32 and the result is rounded once.
+// are multiplied onto the sum in float32, the row's first, and the result is rounded once.
 //
 // Rows and weights are row-major.  v_mfma_i32_16x16x64_i8 takes 16 bytes of
 // one row from each lane (row lane % 16, columns 16 (lane / 16) .. + 15 of 64),
@@ -31,6 +31,10 @@ __device__ __forceinline__ void put4(f16_t* p, const float (&v)[4]) {
   *(f16x4_t*)p = f16x4_t{(f16_t)v[0], (f16_t)v[1], (f16_t)v[2], (f16_t)v[3]};
 }
 
+// A sum with its scales.  The product of the two scales can leave the float32 range where
+// the result does not (0 times infinity, or a result of 0), so it is not formed.
+__device__ __forceinline__ float scaled(int sum, float sa, float sw) { return (float)sum * sa * sw; }
+
 // Where a result goes.
 struct I8Out {
   void* p;
@@ -44,7 +48,7 @@ struct I8Out {
     else ((f16_t*)p)[i] = (f16_t)v;
   }
   __device__ __forceinline__ void store(int m, int n, int acc) const {
-    put((size_t)m * N + n, (float)acc * (sa[m] * sw[n]));
+    put((size_t)m * N + n, scaled(acc, sa[m], sw[n]));
   }
   // scales of columns n .. n + 3 (those past the last are not used)
   __device__ __forceinline__ void scales4(int n, float (&s)[4]) const {
@@ -56,7 +60,7 @@ struct I8Out {
     const size_t i = (size_t)m * N + n;
     float v[4];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) v[r] = (float)acc[r] * (sm * s[r]);
+    for (int r = 0; r < 4; ++r) v[r] = scaled(acc[r], sm, s[r]);
     if (vec && n < N) {
       if (dtype == 0) put4((float*)p + i, v);
       else if (dtype == 1) put4((bf16_t*)p + i, v);
@@ -104,7 +108,7 @@ __device__ __forceinline__ void rows_out(T* p, const i32x4_t (&acc)[FM][FN], int
     for (int j = 0; j < FN; ++j) {
       float v[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) v[r] = (float)acc[i][j][r] * (sc.m[i] * sc.n[j][r]);
+      for (int r = 0; r < 4; ++r) v[r] = scaled(acc[i][j][r], sc.m[i], sc.n[j][r]);
       put4(p + 16 * j, v);
     }
   }
@@ -121,7 +125,7 @@ __device__ __forceinline__ void rows_edge(T* p, bool bf, const i32x4_t (&acc)[FM
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         if (n + 16 * j + r >= N) continue;
-        const float v = (float)acc[i][j][r] * (sc.m[i] * sc.n[j][r]);
+        const float v = scaled(acc[i][j][r], sc.m[i], sc.n[j][r]);
         if constexpr (std::is_same<T, float>::value) p[16 * j + r] = v;
         else p[16 * j + r] = bf ? f2bf(v) : __builtin_bit_cast(uint16_t, (f16_t)v);
       }
