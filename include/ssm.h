@@ -367,7 +367,8 @@ int32_t ssm_gather_rows(int32_t batch, int32_t src_rows, int32_t width, const vo
  * product as the next norm's delta; ssm_quant_i8 also turns weights [out, in]
  * into codes with a scale for each output channel, once, and attention's
  * output into the input of its projection.
- * rows up to 2^24 and may be 0 (nothing is launched), d up to 2^30; arrays are
+ * rows up to 2^24 (of ssm_gemm_i8 up to 64 * 65535, SSM_E_UNSUPPORTED above) and may
+ * be 0 (nothing is launched), d up to 2^30, n up to 2^24; arrays are
  * contiguous, of any alignment their type allows, and do not overlap but where a
  * call says so.
  */

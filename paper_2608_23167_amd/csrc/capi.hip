@@ -584,7 +584,7 @@ int32_t ssm_gather_rows(int32_t batch, int32_t src_rows, int32_t width, const vo
 // Element types of the 8-bit projections' inputs and outputs.
 static bool float_dtype(int32_t dt) { return dt == SSM_DT_F32 || dt == SSM_DT_BF16 || dt == SSM_DT_F16; }
 
-// Rows are dealt out one workgroup each, so their number is a grid size.
+// Row numbers times widths are formed in 64 bits, rows times threads of a launch by launch_rows.
 static constexpr int32_t I8_MAX_ROWS = 1 << 24;
 // Sums of K products of codes in [-128, 127] stay below 2^31.
 static constexpr int32_t I8_MAX_K = (1 << 17) - 1;
@@ -621,7 +621,8 @@ static int32_t check_gemm_i8(int32_t m, int32_t n, int32_t k) {
   if (m < 0 || m > I8_MAX_ROWS || n < 1 || n > I8_MAX_ROWS || k < 1)
     return fail(SSM_E_INVAL, "bad sizes (m %d, n %d, k %d)", m, n, k);
   if (k > I8_MAX_K) return fail(SSM_E_UNSUPPORTED, "k %d above %d: an int32 sum could overflow", k, I8_MAX_K);
-  // the grid of the kernel for any alignment has ceil(m / 64) workgroups in y
+  // the grid of the kernel for any alignment has ceil(m / 64) workgroups in y; the tiles of
+  // what fits the memory of the card are far fewer than a launch holds
   if (m > 64 * 65535) return fail(SSM_E_UNSUPPORTED, "m %d above %d rows", m, 64 * 65535);
   return SSM_OK;
 }

@@ -32,6 +32,24 @@ inline void launch(void (*kernel)(KArgs...), dim3 grid, dim3 block, uint32_t shm
   if (timed) hipEventRecord(b, st);
 }
 
+// A launch holds fewer than 2^32 threads along an axis: the rows that one takes at
+// `rows_per_wg` rows to a workgroup of `threads` threads.
+constexpr int64_t rows_a_launch(int threads, int rows_per_wg) {
+  return ((1ll << 32) - 1) / threads * rows_per_wg;
+}
+// Calls go(first row, rows) for as few launches as `rows` rows need, up to the first that fails.
+template <class Go> inline hipError_t launch_rows(int rows, int threads, int rows_per_wg, Go go) {
+  const int64_t most = rows_a_launch(threads, rows_per_wg);
+  for (int at = 0; at < rows;) {
+    const int n = rows - at < most ? rows - at : (int)most;
+    go(at, n);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    at += n;
+  }
+  return hipSuccess;
+}
+
 // Left padding of each sequence of a batch whose prompts differ in length.
 // The batch shares one row layout, that of its longest prompt; sequence s,
 // whose prompt is pad[s] tokens shorter, sits pad[s] positions to the left

@@ -336,15 +336,21 @@ hipError_t launch_token_logprobs(int dtype, int rows, int V, const void* logits,
   auto go = [&](auto* x) {
     using T = std::remove_cv_t<std::remove_pointer_t<decltype(x)>>;
     const auto rows_by = [&](auto kernel) {
-      launch(kernel, dim3(rows * p.parts), dim3(64 * p.waves), 0, st, x, V, mask_id, n_targets, targets, k,
-             p.parts, p.chunk, lp, entropy, top_ids, top_lp, part);
+      return launch_rows(rows, 64 * p.waves * p.parts, 1, [&](int at, int n) {
+        const size_t r = at;
+        launch(kernel, dim3(n * p.parts), dim3(64 * p.waves), 0, st, x + r * V, V, mask_id, n_targets,
+               targets ? targets + r * n_targets : targets, k, p.parts, p.chunk, lp ? lp + r * n_targets : lp,
+               entropy ? entropy + r : entropy, top_ids ? top_ids + r * k : top_ids, top_lp ? top_lp + r * k : top_lp,
+               part);                              // rows in parts are few: one launch
+      });
     };
-    if (p.waves == 1) rows_by(logprobs_kernel<T, 1>);
-    else if (p.waves == 16) rows_by(logprobs_kernel<T, 16>);
-    else rows_by(logprobs_kernel<T, 4>);
-    if (p.parts > 1)
-      launch(logprobs_join_kernel<T>, dim3(rows), dim3(64), 0, st, part, p.parts, x, V, mask_id,
-             n_targets, targets, k, lp, entropy, top_ids, top_lp);
+    hipError_t e;
+    if (p.waves == 1) e = rows_by(logprobs_kernel<T, 1>);
+    else if (p.waves == 16) e = rows_by(logprobs_kernel<T, 16>);
+    else e = rows_by(logprobs_kernel<T, 4>);
+    if (e != hipSuccess || p.parts == 1) return e;
+    launch(logprobs_join_kernel<T>, dim3(rows), dim3(64), 0, st, part, p.parts, x, V, mask_id,
+           n_targets, targets, k, lp, entropy, top_ids, top_lp);
     return hipGetLastError();
   };
   if (dtype == 0) return go((const float*)logits);

@@ -217,7 +217,7 @@ template <typename T> struct SwigluValue {        // gate in [0, d), up in [d, 2
 
 // One workgroup per row, any width and alignment: the row is read twice.
 template <typename T, bool SWIGLU>
-__global__ void __launch_bounds__(256) quant_i8_kernel(const T* __restrict__ x, int d,
+__global__ void __launch_bounds__(256) quant_i8_kernel(const T* __restrict__ x, int rows, int d,
                                                        int8_t* __restrict__ q,
                                                        float* __restrict__ scale) {
   __shared__ uint32_t red[4];
@@ -237,7 +237,7 @@ __global__ void __launch_bounds__(256) quant_i8_kernel(const T* __restrict__ x, 
 // last pass reads each element before it writes it.
 template <typename TD, typename TG>
 __global__ void __launch_bounds__(256) norm_i8_kernel(const float* x, const TD* delta,
-                                                      const TG* __restrict__ g, int d, float eps,
+                                                      const TG* __restrict__ g, int rows, int d, float eps,
                                                       float* resid, int8_t* __restrict__ q,
                                                       float* __restrict__ scale) {
   __shared__ float red[4];
@@ -282,13 +282,16 @@ static bool aligned(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes
 template <typename T>
 static hipError_t quant_t(int rows, int d, bool sw, const T* x, int8_t* q, float* scale, hipStream_t st) {
   const bool vec = d % 4 == 0 && aligned(x, 4 * sizeof(T)) && aligned(q, 4);
-#define QUANT(V, NV, TPR)                                                                            \
-  do {                                                                                               \
-    const dim3 grid(ceil_div(rows, TPR < 256 ? 256 / TPR : 1)), block(TPR < 256 ? 256 : TPR);        \
-    if (sw) launch((quant_rows_kernel<T, true, V, NV, TPR>), grid, block, 0, st, x, rows, d, q, scale); \
-    else launch((quant_rows_kernel<T, false, V, NV, TPR>), grid, block, 0, st, x, rows, d, q, scale);   \
-    return hipGetLastError();                                                                        \
-  } while (0)
+  const size_t width = sw ? (size_t)2 * d : d;
+  const auto by_rows = [&](auto plain, auto gated, int threads, int rows_per_wg) {
+    return launch_rows(rows, threads, rows_per_wg, [&](int at, int n) {
+      launch(sw ? gated : plain, dim3(ceil_div(n, rows_per_wg)), dim3(threads), 0, st, x + at * width, n, d,
+             q + (size_t)at * d, scale + at);
+    });
+  };
+#define QUANT(V, NV, TPR)                                                                         \
+  return by_rows(quant_rows_kernel<T, false, V, NV, TPR>, quant_rows_kernel<T, true, V, NV, TPR>, \
+                 TPR < 256 ? 256 : TPR, TPR < 256 ? 256 / TPR : 1)
   if constexpr (sizeof(T) == 2) {                  // 16-byte loads of 16-bit rows
     if (d % 8 == 0 && aligned(x, 16) && aligned(q, 8)) {
       if (d <= 1024) QUANT(8, 2, 64);
@@ -300,9 +303,7 @@ static hipError_t quant_t(int rows, int d, bool sw, const T* x, int8_t* q, float
   }
   ROWS_DISPATCH(QUANT);
 #undef QUANT
-  if (sw) launch(quant_i8_kernel<T, true>, dim3(rows), dim3(256), 0, st, x, d, q, scale);
-  else launch(quant_i8_kernel<T, false>, dim3(rows), dim3(256), 0, st, x, d, q, scale);
-  return hipGetLastError();
+  return by_rows(quant_i8_kernel<T, false>, quant_i8_kernel<T, true>, 256, 1);
 }
 
 hipError_t launch_quant_i8(int dtype, int rows, int d, bool swiglu, const void* x, int8_t* q,
@@ -318,16 +319,18 @@ static hipError_t norm_t(int rows, int d, const float* x, const TD* delta, const
                          float* resid, int8_t* q, float* scale, hipStream_t st) {
   const bool vec = d % 4 == 0 && aligned(x, 16) && aligned(g, 4 * sizeof(TG)) && aligned(q, 4) &&
                    aligned(delta, 4 * sizeof(TD)) && aligned(resid, 16);
-#define NORM(V, NV, TPR)                                                                        \
-  do {                                                                                          \
-    launch((norm_rows_kernel<TD, TG, V, NV, TPR>), dim3(ceil_div(rows, TPR < 256 ? 256 / TPR : 1)), \
-           dim3(TPR < 256 ? 256 : TPR), 0, st, x, delta, g, rows, d, eps, resid, q, scale);     \
-    return hipGetLastError();                                                                   \
-  } while (0)
+  const auto by_rows = [&](auto kernel, int threads, int rows_per_wg) {
+    return launch_rows(rows, threads, rows_per_wg, [&](int row, int n) {
+      const size_t at = (size_t)row * d;
+      launch(kernel, dim3(ceil_div(n, rows_per_wg)), dim3(threads), 0, st, x + at, delta ? delta + at : delta, g,
+             n, d, eps, resid ? resid + at : resid, q + at, scale + row);
+    });
+  };
+#define NORM(V, NV, TPR) \
+  return by_rows(norm_rows_kernel<TD, TG, V, NV, TPR>, TPR < 256 ? 256 : TPR, TPR < 256 ? 256 / TPR : 1)
   ROWS_DISPATCH(NORM);
 #undef NORM
-  launch(norm_i8_kernel<TD, TG>, dim3(rows), dim3(256), 0, st, x, delta, g, d, eps, resid, q, scale);
-  return hipGetLastError();
+  return by_rows(norm_i8_kernel<TD, TG>, 256, 1);
 }
 template <typename TG>
 static hipError_t norm_g(int delta_dtype, int rows, int d, const float* x, const void* delta,
@@ -347,3 +350,10 @@ hipError_t launch_norm_i8(int rows, int d, const float* x, const void* delta, in
 }
 
 }  // namespace ssm
+
+// The rows of one launch, for tests.
+#ifdef SSM_DEBUG
+extern "C" int64_t ssm_debug_rows_a_launch(int32_t threads, int32_t rows_per_wg) {
+  return ssm::rows_a_launch(threads, rows_per_wg);
+}
+#endif
