@@ -216,13 +216,17 @@ def _arg(t: Optional[torch.Tensor], dtype, name: str) -> Optional[int]:
 
 
 def _on(stream, *tensors: Optional[torch.Tensor]) -> int:
-    """The stream's handle.  The library launches on the current device: tensors of
-    another are refused."""
+    """The stream's handle.  The library launches on the current device: tensors and
+    streams of another are refused."""
     dev = torch.cuda.current_device()
     for t in tensors:
         if t is not None and t.get_device() != dev:
             raise ValueError(f"tensors must be on the current device (cuda:{dev}), got {t.device}")
-    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(dev)
+    if stream.device_index != dev:
+        raise ValueError(f"stream must be of the current device (cuda:{dev}), got cuda:{stream.device_index}")
+    return stream.cuda_stream
 
 
 def ssm_norm_i8(x: torch.Tensor, gain: torch.Tensor, eps: float, q: torch.Tensor,
