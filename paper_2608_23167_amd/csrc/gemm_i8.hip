@@ -10,6 +10,7 @@
 #include <stdio.h>
 #include <stdlib.h>
 
+#include "dcheck.h"
 #include "internal.h"
 #include "tiles.h"
 
@@ -185,6 +186,7 @@ __global__ void __launch_bounds__(256) gemm_i8_any_kernel(const int8_t* __restri
   const int r16 = lane & 15, q = lane >> 4;
   const int M = out.M, N = out.N, m0 = blockIdx.y * 64, n0 = blockIdx.x * 64;
   const int nk = (K + 127) >> 7;
+  SSM_DCHECK(m0 < M && n0 < N);
   const int8_t* src[2][2];
   int dst[2], col[2];
 #pragma unroll
@@ -260,6 +262,7 @@ __global__ void __launch_bounds__(512) gemm_i8_few_kernel(const int8_t* __restri
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r16 = lane & 15, q = lane >> 4;
   const int M = out.M, N = out.N, n0 = blockIdx.x * 16;
+  SSM_DCHECK(M <= 16 && n0 < N && K >= 16 && K % 16 == 0);
   const int steps = (K + 63) >> 6, s0 = wave * steps >> 3, s1 = (wave + 1) * steps >> 3;
   const int8_t* wp = W + (size_t)min(n0 + r16, N - 1) * K;
   const int8_t* ap = A + (size_t)min(r16, M - 1) * K;
@@ -384,6 +387,7 @@ __global__ void __launch_bounds__(512, 2) gemm_i8_pp_kernel(const int8_t* __rest
   const int k_steps = K >> 7;                      // whole ones
   const int ks0 = (int)((long long)split * k_steps / n_split);
   const int nk = (int)((long long)(split + 1) * k_steps / n_split) - ks0, last = nk - 1;   // nk >= 1 (host-checked)
+  SSM_DCHECK(nk >= 1 && m0 < M && n0 < N && (part != nullptr) == (n_split > 1) && ldp >= N);
   const int rot = t % nk;
   auto kmap = [rot, nk](int x) { const int y = x + rot; return y >= nk ? y - nk : y; };
 
@@ -571,6 +575,7 @@ __global__ void __launch_bounds__(512, 2) gemm_i8_ks_kernel(const int8_t* __rest
   const int k_steps = K >> 7;                      // whole ones
   const int ks0 = (int)((long long)split * k_steps / n_split);
   const int nk = (int)((long long)(split + 1) * k_steps / n_split) - ks0, last = nk - 1;   // nk >= 1 (host-checked)
+  SSM_DCHECK(nk >= 1 && m0 < M && n0 < N && (part != nullptr) == (n_split > 1) && ldp >= N);
   const int rot = t % nk;
   auto kmap = [rot, nk](int x) { const int y = x + rot; return y >= nk ? y - nk : y; };
 
@@ -738,6 +743,7 @@ __global__ void __launch_bounds__(512, 2) gemm_i8_ks_kernel(const int8_t* __rest
 template <int S>
 __global__ void __launch_bounds__(256) gemm_i8_sum_kernel(const int* __restrict__ part, int ldp, I8Out out) {
   const int n = 4 * (int)(blockIdx.x * 256 + threadIdx.x);
+  SSM_DCHECK(ldp >= out.N);
   if (n >= out.N) return;
   float s[4];
   out.scales4(n, s);

@@ -8,6 +8,7 @@
 // Logits of -inf (and the [MASK] id, which counts as one) add nothing.  A row
 // with a NaN or a +inf, or with nothing above -inf, has an m that is not
 // finite, and m - m makes its log probabilities and entropy NaN.
+#include "dcheck.h"
 #include "internal.h"
 #include "row_stats.h"
 
@@ -118,6 +119,7 @@ __device__ __forceinline__ void row_results(size_t row, const Soft& s, const T* 
     lp[row * n_targets + i] = r;
   }
   merge_lists(k, next, [&](int q, float v, int i) {
+    SSM_DCHECK(i == STAT_NONE || (i >= 0 && i < V && i != mask_id));
     if (lane == 0) {
       top_ids[row * k + q] = i == STAT_NONE ? -1 : i;
       top_lp[row * k + q] = i == STAT_NONE ? -INFINITY : ((v - s.m) - lz) + spoilt;
@@ -157,6 +159,7 @@ __global__ void __launch_bounds__(64 * NW) logprobs_kernel(
   const int p = blockIdx.x % parts;
   const T* L = logits + row * V;
   const int lo = p * chunk, hi = min(V, lo + chunk);
+  SSM_DCHECK(k <= STAT_K && lo < hi);
   const int skew = (int)(((uintptr_t)(L + lo) & 15) / sizeof(T));
   const int body = min(hi, lo + (skew ? VE - skew : 0));       // first aligned column
   const int tiles = (hi - body) / TILE, tail = body + tiles * TILE;
@@ -283,6 +286,7 @@ __global__ void __launch_bounds__(64) logprobs_join_kernel(
     float* __restrict__ entropy, int32_t* __restrict__ top_ids, float* __restrict__ top_lp) {
   const int lane = threadIdx.x;
   const size_t row = blockIdx.x;
+  SSM_DCHECK(parts <= 64);
   const Part* mine = in + row * parts + lane;
   Soft s{-INFINITY, 0.f, 0.f};
   if (lane < parts) s = mine->s;

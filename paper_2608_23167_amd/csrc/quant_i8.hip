@@ -6,6 +6,7 @@
 // I8_TINY (rows of zeros among them) gets scale 0 and codes 0: 127 / max|y|
 // would leave the float32 range there.  A row with an infinity or a NaN gets
 // scale NaN and codes 0, so that whatever is computed from it is NaN.
+#include "dcheck.h"
 #include "internal.h"
 
 namespace ssm {
@@ -114,6 +115,7 @@ quant_rows_kernel(const T* __restrict__ x, int rows, int d, int8_t* __restrict__
   constexpr int RPB = TPR < 256 ? 256 / TPR : 1;
   __shared__ float red[16];
   __shared__ uint32_t redu[16];
+  SSM_DCHECK(d <= V * NV * TPR && d % V == 0);
   const int t = threadIdx.x % TPR;
   const size_t row = (size_t)blockIdx.x * RPB + threadIdx.x / TPR;
   if (row >= (size_t)rows) return;                  // whole waves, and only where a wave is a row
@@ -155,6 +157,7 @@ norm_rows_kernel(const float* x, const TD* delta, const TG* __restrict__ g, int 
   constexpr int RPB = TPR < 256 ? 256 / TPR : 1;
   __shared__ float red[16];
   __shared__ uint32_t redu[16];
+  SSM_DCHECK(d <= V * NV * TPR && d % V == 0);
   const int t = threadIdx.x % TPR;
   const size_t row = (size_t)blockIdx.x * RPB + threadIdx.x / TPR;
   if (row >= (size_t)rows) return;
