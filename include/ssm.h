@@ -358,9 +358,10 @@ int32_t ssm_gather_rows(int32_t batch, int32_t src_rows, int32_t width, const vo
 /*
  * Codes and scales.  A row y becomes scale = max|y| / 127 (float32) and codes
  * q = round(y / scale), to nearest even, in [-127, 127], so that q * scale is
- * within half a step of y.  A row whose largest magnitude is below 2^-100 (a
- * row of zeros, for one) gets scale 0 and codes 0; a row with an infinity or a
- * NaN gets scale NaN and codes 0, so that what is computed from it is NaN.
+ * within half a step of y, up to the float32 roundings of y * (127 / max|y|).  A
+ * row whose largest magnitude is below 2^-100 (a row of zeros, for one) gets scale
+ * 0 and codes 0; a row with an infinity or a NaN gets scale NaN and codes 0, so
+ * that what is computed from it is NaN.
  * A feed-forward block in 8 bits is
  *   ssm_norm_i8 -> ssm_gemm_i8 (gate and up weights, one above the other)
  *   -> ssm_quant_i8 with swiglu -> ssm_gemm_i8 (down) -> ssm_norm_i8 with the
@@ -428,7 +429,7 @@ int32_t ssm_token_logprobs_workspace_size(int32_t rows, int32_t vocab, int32_t k
 
 /*
  * For each row of logits d_logits [rows, vocab] (dtype SSM_DT_F32, BF16 or F16:
- * the logits of ssm_denoise_step, or those of an 8-bit head), with p the
+ * those of an 8-bit head, or ssm_denoise_step's d_logits_dbg), with p the
  * softmax over the vocabulary without mask_id (-1: nothing is left out):
  *   d_logprob     float32 [rows, n_targets]: ln p of the tokens d_targets int32
  *                 [rows, n_targets]; -inf for mask_id, NaN for an id outside

@@ -254,7 +254,7 @@ __global__ void __launch_bounds__(256) gemm_i8_any_kernel(const int8_t* __restri
 // of the K-steps of 64 and reads its operands straight from memory (no operand is
 // read by two waves of a workgroup); the eight partial sums join in LDS.  Bound by
 // the weights' bytes: each wave keeps two batches of U K-steps in flight.  One row of
-// 4096 x 4096: 6.0 us (2.8 TB/s; launch and one trip to memory are 4 of them).
+// 4096 x 4096: 6.5 us (2.6 TB/s; launch and one trip to memory are 4 of them).
 template <int U>
 __global__ void __launch_bounds__(512) gemm_i8_few_kernel(const int8_t* __restrict__ A,
                                                           const int8_t* __restrict__ W, int K, I8Out out) {
@@ -337,8 +337,8 @@ __global__ void __launch_bounds__(512) gemm_i8_few_kernel(const int8_t* __restri
 // 16-19 and 28-31) together, which counters say is how they go: with r / 4 for
 // half_place(r), even for the first grouping only, 13% of the clocks were conflicts.
 // What is left of K past the last whole K-step is multiplied from registers.
-// 3840 x 24576 x 4096: 356 us, 2170 TOP/s; the MFMAs are busy 53% of the clocks, and the
-// clock gives way to the power of that (1.9 GHz).  Of a round of 61 us 10 pass before the
+// 3840 x 24576 x 4096: 350-357 us, 2190 TOP/s; the MFMAs are busy 51% of the clocks, at 1.97
+// GHz (kernels that wait for memory run at 2.3 and more).  Of a round of 61 us 10 pass before the
 // first product and after the last; workgroups that stay for several tiles and start
 // the next one's copies before they store were tried: the loop around it all spilled.
 __device__ __forceinline__ int half_place(int r) {      // 0, 2, 3, 1 for r / 4 = 0 .. 3
@@ -347,8 +347,9 @@ __device__ __forceinline__ int half_place(int r) {      // 0, 2, 3, 1 for r / 4 
 
 // tile_of with the row tiles in groups of 4, innermost in a group: the 32 tiles that an XCD
 // works on at a time are then about 4 x 8 and need 12 strips of rows and weights in its
-// L2, where 15 x 2 need 17.  3840 x 24576 x 4096 371 -> 363 us, 3840 x 12288 x 4096 182 -> 174,
-// 14208 x 24576 x 4096 1297 -> 1222 (2340 TOP/s); groups of 8 368, 175 and 1273.
+// L2, where 15 x 2 need 17, and 3840 x 24576 x 4096 fetches 629 instead of 1192 MiB.  That
+// one takes as long either way (351 and 354 us in turn); 3840 x 12288 x 4096 180 -> 173, 14208 x
+// 24576 x 4096 1300 -> 1215 (2350 TOP/s); groups of 8 360, 175 and 1275.
 __device__ __forceinline__ void grouped_tile_of(int w, int total, int ntm, int mt, int& split, int& tn,
                                                 int& tm) {
   constexpr int GROUP = 4;
@@ -767,9 +768,12 @@ __global__ void __launch_bounds__(256) gemm_i8_sum_kernel(const int* __restrict_
 // each of the 256 CUs (one fits a CU).  In a round of w workgroups a K-step of 128
 // takes step + fill * w / 256 us, the second part for what the CUs share, but the
 // weights come no faster than I8_HBM bytes a us; `fixed` is what a round takes besides.
-// Measured on 160 sizes (40-3840 rows, 700-126464 columns, K 1024-18944) times 12
-// tiles times 6 splits, the weights from memory: the choice takes 0.4% more than
-// the best of them in the mean, 12% at most.  The kernel for few rows took 7.3 us for
+// The coefficients were fitted to 161 sizes (40-3840 rows, 700-126464 columns, K 1024-18944) times
+// 12 tiles times 6 splits, the weights from memory, before grouped_tile_of: there the choice
+// took 0.4% more than the best in the mean, 12% at most.  On 70 other sizes drawn over 17-4000
+// rows, 500-40000 columns and K 1024-18944 it takes 2.5% more in the mean, above 5% on 14 of them
+// and 24% at most (256 x 192 tiles for 2383 x 10205 x 1200, 101 us, where 128 x 256 take 81).  In
+// rows of launches, with what lies between them, the kernel for few rows took 7.3 us for
 // one row of 4096 x 4096 (64 x 32 tiles 10.3), 12.5 of 4096 x 12288 (15.1), but 27.7 of
 // 24576 x 4096 (64 x 96 tiles 20.4), and for 16 rows 8.6, 17.4 and 38.6 (10.1, 15.5, 20.8).
 static constexpr int I8_FEW_ROWS = 16;

@@ -144,8 +144,8 @@ __device__ __forceinline__ void row_results(size_t row, const Soft& s, const T* 
 // it, as in the first tile or in rising rows, the k-th largest of the lanes'
 // maxima is a floor for this tile's candidates.  Each candidate then goes to its
 // place in the list by value and id; one that finds none takes along all that
-// are no better than the k-th (3840 rows of 126464 bfloat16 logits, k = 8: random 217 us,
-// all equal 180, without this 867; rising 920, without 3637).
+// are no better than the k-th (3840 rows of 126464 bfloat16 logits, k = 8: random 190-195 us
+// and 175 with k = 0; all equal 180, without this 867; rising 915, without 3637).
 template <typename T, int NW>
 __global__ void __launch_bounds__(64 * NW) logprobs_kernel(
     const T* __restrict__ logits, int V, int mask_id, int n_targets,
@@ -305,9 +305,13 @@ __global__ void __launch_bounds__(64) logprobs_join_kernel(
 //    0.68 us a million of all rows' columns.  Measured, float32: one row of 16384 8.0
 //    against 10.5 us, of 65536 14.9 against 10.7; 120 rows of 32768 12.8 against 14.7;
 //    240 rows of 126464 27.6 against 31.6.
-//  * Else workgroups of 4 waves; whole rows once there are 385, below in parts of at least a
-//    tile to each wave, 768 workgroups, 3 to a CU: 120 rows of 126464 in 6 parts 23.9 us, in
-//    8 23.5; 400 rows whole 43.4, in 2 parts 46.9.
+//  * Else workgroups of 4 waves; whole rows once there are 385, below in as many parts as
+//    768 workgroups, 3 to a CU, have rows, of at least a tile to each wave.  A part is a
+//    multiple of 4096 columns, a tile to each wave, so there are fewer parts than that
+//    where V / 4096 is near their number, and the last holds what is left: one row of
+//    152064 columns is 18 parts of 8192 and one of 4608, 120 rows of 126464 are 5 parts
+//    of 24576 and one of 3584 each.  120 rows of 126464 in 6 parts 23.9 us, in 8 23.5 (k = 5,
+//    which is 10 us of it: 13.8 with k = 0); 400 rows whole 43.4, in 2 parts 46.9.
 struct LogprobsPlan {
   int waves, parts, chunk;
 };

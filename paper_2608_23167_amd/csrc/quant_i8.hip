@@ -54,10 +54,12 @@ __device__ __forceinline__ float swiglu(float g, float u) { return g / (1.f + ex
 // 256 or 1024: the workgroup), NV pieces of V elements to a thread, piece
 // number t + TPR i of the row.  Every element is read once, the row's sum and
 // largest magnitude are reduced together, and the codes leave from registers.
-// Bound by memory: the norm of 14208 x 4096 with a float32 residual 135 us (757 MB at
-// 5.6 TB/s; read three times by one workgroup a row 290), 5081 x 3584 float32 rows
-// 16.3 us (5.6 TB/s), 12288 x 4096 bfloat16 weights 23.5 us (6.4 TB/s); few rows by the
-// launch and two trips to memory: SwiGLU of 240 x 12288 6.5 us, the norm of one row 3.4.
+// Bound by memory: the norm of 14208 x 4096 with a float32 residual 137 us (757 MB at
+// 5.5 TB/s; read three times by one workgroup a row 290), 5081 x 3584 float32 rows
+// 16.6 us (5.5 TB/s), 12288 x 4096 bfloat16 weights 28 us (5.4 TB/s); few rows by the
+// launch and two trips to memory: SwiGLU of 240 x 12288 6.2 us, the norm of one row 3.6.
+// SwiGLU of many 16-bit rows by the vector ALUs (an exponential and a division an element):
+// 3840 x 12288 bfloat16 52 us (4.6 TB/s), the ALUs busy 92% of the clocks; float32 83 (5.1).
 template <int V, typename T> __device__ __forceinline__ void load_v(const T* p, float (&v)[V]) {
   if constexpr (V == 1) {
     v[0] = ldf(p);
